@@ -67,7 +67,8 @@ enum {
 
 enum { SALUS_JOB_QUEUED = 0, SALUS_JOB_RESIDENT = 1, SALUS_JOB_EVICTED = 2, SALUS_JOB_DONE = 3 };
 
-enum { SALUS_ACT_NONE = 0, SALUS_ACT_RELU = 1, SALUS_ACT_GELU = 2 };
+/* SILU: z / (1 + exp(-z)), for the calls on gated blocks and dense layers with bias and residual. */
+enum { SALUS_ACT_NONE = 0, SALUS_ACT_RELU = 1, SALUS_ACT_GELU = 2, SALUS_ACT_SILU = 3 };
 
 enum { SALUS_F32 = 0, SALUS_BF16 = 1 };
 
@@ -326,6 +327,106 @@ uint64_t salus_train_work_bytes(uint32_t M, const salus_train_layer *layers, uin
  * salus_grouped_forward; K and N multiples of 8. */
 int32_t salus_grouped_train_step(salus_pool_t *pool, const salus_train_desc *descs, uint32_t n,
                                  void *stream);
+
+/* ---- transformer blocks -------------------------------------------------------
+ * Gated feed-forward blocks and dense layers with bias, activation and residual,
+ * forward and backward, and gradient clipping, as packed calls: all n jobs
+ * together on `stream`, asynchronously, under the residency, lane and bounds
+ * rules of salus_grouped_forward (pairwise different lanes, every buffer inside the
+ * lane or the persistent block).  All matrices are row-major, inputs and weights bf16; sums
+ * are float.  K, F and N are positive multiples of 8 below 2^22 (2 F as well), M
+ * is at least 1; offsets are multiples of 16.  What is written may overlap nothing else of
+ * the job's call, except that y may be r itself where y is bf16 (a residual
+ * stream updated in place); what is only read may coincide (x and r).  The calls
+ * are plain kernel launches with by-value arguments and can be recorded in a graph;
+ * a result does not depend on the other jobs' data, nor on atomics. */
+
+/* An offset that is not given. */
+#define SALUS_ABSENT UINT64_MAX
+
+/* Y = (act(X Wg) * (X Wu)) Wout + R.  In the persistent block: w_in, K x 2F, the F
+ * columns of Wg in front of those of Wu; w_out, F x N.  In the lane: x M x K; y M x N bf16;
+ * h M x F bf16, written: the hidden activations, rounded for the second product and needed by the
+ * backward pass; r M x N bf16 or SALUS_ABSENT; gu M x 2F float, written if not SALUS_ABSENT:
+ * [X Wg, X Wu], needed by the backward pass. */
+typedef struct {
+    int32_t  job;
+    uint32_t M, K, F, N;
+    int32_t  act;          /* SALUS_ACT_* */
+    uint64_t w_in_off, w_out_off;
+    uint64_t x_off, y_off, h_off, r_off, gu_off;
+} salus_gated_desc;
+int32_t salus_grouped_gated_forward(salus_pool_t *pool, const salus_gated_desc *descs, uint32_t n,
+                                    void *stream);
+
+/* Its gradients, from dy M x N bf16 and what the forward pass left in x, h and gu:
+ *   dH = dY Wout^T, [dG dU] = bf16[dH * U * act'(G), dH * act(G)];
+ *   dX = [dG dU] Win^T (M x K; not computed if dx_off is SALUS_ABSENT);
+ *   dWin = X^T [dG dU] (K x 2F), dWout = H^T dY (F x N),
+ * all bf16 in the lane.  (The residual's gradient is dy.)  work: salus_gated_grad_work_bytes(). */
+typedef struct {
+    int32_t  job;
+    uint32_t M, K, F, N;
+    int32_t  act;
+    uint64_t w_in_off, w_out_off;
+    uint64_t x_off, h_off, gu_off, dy_off, dx_off, dw_in_off, dw_out_off, work_off;
+} salus_gated_grad_desc;
+uint64_t salus_gated_grad_work_bytes(uint32_t M, uint32_t F);
+int32_t salus_grouped_gated_backward(salus_pool_t *pool, const salus_gated_grad_desc *descs, uint32_t n,
+                                     void *stream);
+
+/* Y = act(X W + b) + R.  In the persistent block: w K x N, b N bf16 or SALUS_ABSENT.  In the lane:
+ * x M x K; y M x N of y_dtype; r M x N bf16 or SALUS_ABSENT; z M x N float,
+ * written if not SALUS_ABSENT: X W + b, needed by the backward pass unless act is NONE. */
+typedef struct {
+    int32_t  job;
+    uint32_t M, K, N;
+    int32_t  act;
+    int32_t  y_dtype;      /* SALUS_BF16 or SALUS_F32 */
+    uint64_t w_off, b_off;
+    uint64_t x_off, y_off, r_off, z_off;
+} salus_dense_desc;
+int32_t salus_grouped_dense_forward(salus_pool_t *pool, const salus_dense_desc *descs, uint32_t n,
+                                    void *stream);
+
+/* Its gradients: dZ = dY * act'(Z); dX = dZ W^T (M x K, or SALUS_ABSENT), dW = X^T dZ (K x N), bf16;
+ * db (N floats, or SALUS_ABSENT): column sums of dZ in float.  The products take dZ
+ * rounded to bf16.  z_off is SALUS_ABSENT exactly if act is NONE. */
+typedef struct {
+    int32_t  job;
+    uint32_t M, K, N;
+    int32_t  act;
+    uint64_t w_off;
+    uint64_t x_off, z_off, dy_off, dx_off, dw_off, db_off, work_off;
+} salus_dense_grad_desc;
+uint64_t salus_dense_grad_work_bytes(uint32_t M, uint32_t N);
+int32_t salus_grouped_dense_backward(salus_pool_t *pool, const salus_dense_grad_desc *descs, uint32_t n,
+                                     void *stream);
+
+/* Global gradient norm over all of a job's tensors, and clipping:
+ *   norm = sqrt(sum g^2), c = min(1, max_norm / norm) (NaN if the norm is),
+ *   salus_grouped_clip:      g <- c g (rounded to g's type; untouched if c is 1)
+ *   salus_grouped_clip_sgd:  wm <- wm - lr (c g), wb <- bf16(wm); g is left as it is
+ * g: count elements (at least 1, below 2^48) of dtype in the lane; wm float, wb bf16, count elements each in the
+ * persistent block (not used by salus_grouped_clip).  norm: one float in the lane, written.  Sums are kept in 64
+ * bits, in an order that depends on the counts alone.  max_norm > 0 (infinity: nothing is
+ * scaled); work: salus_clip_work_bytes(). */
+typedef struct {
+    uint64_t g_off, count;
+    uint64_t wm_off, wb_off;
+    int32_t  dtype;        /* SALUS_F32 or SALUS_BF16: of g */
+    int32_t  pad;
+} salus_clip_tensor;
+typedef struct {
+    int32_t  job;
+    uint32_t n_tensors;
+    const salus_clip_tensor *tensors;      /* host pointer, n_tensors entries */
+    float    max_norm, lr;
+    uint64_t norm_off, work_off;
+} salus_clip_desc;
+uint64_t salus_clip_work_bytes(const salus_clip_tensor *tensors, uint32_t n_tensors);
+int32_t salus_grouped_clip(salus_pool_t *pool, const salus_clip_desc *descs, uint32_t n, void *stream);
+int32_t salus_grouped_clip_sgd(salus_pool_t *pool, const salus_clip_desc *descs, uint32_t n, void *stream);
 
 /* Efficient job switching made explicit for jobs that cannot stay
  * (Sections 3.2 and 4.2): RESIDENT -> EVICTED copies the persistent block to

@@ -11,6 +11,7 @@
 #include <string>
 #include <vector>
 
+#include "api.hpp"
 #include "device.hpp"
 #include "pool_core.hpp"
 #include "salus.h"
@@ -161,6 +162,32 @@ static int32_t done(salus_pool *p, int32_t rc)
     p->device_error.clear();
     return rc;
 }
+
+namespace salus {
+
+int32_t pool_error(salus_pool *pool, int32_t code, const char *message) { return set_error(pool, code, message); }
+
+int32_t place_job(salus_pool *pool, int32_t job, std::vector<int32_t> &lanes_used, Placed *out)
+{
+    const Job *j = pool->core->job(job);
+    if (!j) return set_error(pool, SALUS_EINVAL, "descriptor names an unknown job");
+    if (j->state != SALUS_JOB_RESIDENT) return set_error(pool, SALUS_ENOTRESIDENT, "job " + std::to_string(job) + " is not resident");
+    if (j->held) return set_error(pool, SALUS_EBUSY, "job " + std::to_string(job) + " is in transit");
+    if (std::find(lanes_used.begin(), lanes_used.end(), j->lane) != lanes_used.end())
+        return set_error(pool, SALUS_EBUSY, "two jobs of lane " + std::to_string(j->lane) + " in one packed iteration");
+    lanes_used.push_back(j->lane);
+    const uint64_t lane_off = pool->core->lane_base(j->lane, &out->lane_size);
+    out->persist = pool->ops.base + j->off;
+    out->lane = pool->ops.base + lane_off;
+    out->P = j->P;
+    return SALUS_OK;
+}
+
+bool has_device(const salus_pool *pool) { return pool->ops.present(); }
+bool weights_cached(const salus_pool *pool) { return pool->core->resident_bytes() <= kCachedBytes; }
+uint64_t *launch_counter(salus_pool *pool) { return &pool->gemm_launches; }
+
+}  // namespace salus
 
 extern "C" {
 

@@ -87,6 +87,7 @@ struct Operand {
     uint32_t extent;      // rows (major) or columns (tr) of the matrix
     uint32_t pitch;       // bytes between rows (major) or between k-rows (tr)
     bool strip;           // tr only: columns in strips of 128, each depth x 128 contiguous
+    uint32_t second = 0;  // PAIRS: bytes from a column to the one it is paired with
 };
 
 // tr: what is xored to the chunks of k-row `row` (64 columns: two k-rows share a 256-byte bank row)
@@ -97,8 +98,11 @@ __device__ inline uint32_t tr_swizzle(uint32_t row) { return B >= 128 ? 4u * (ro
 // 1 KB per slab.  Requests are issued in k-steps 3, 0, 1, 2 (major: a slab, three slabs ahead) or 1, 2 and 3, 0 (tr: the
 // first and the second half of a slab, two slabs ahead) of the slab being multiplied.
 // UNIT: k-values of a stage (a major operand's is a whole slab, the 128 bytes of a line).  ONCE: requests are non-temporal.
-template <int B, bool TR, int WAVES, int STAGES = TR ? 2 : 3, uint32_t UNIT = kSlab, bool ONCE = false>
+// PAIRS (tr): a tile is B / 2 columns and the same ones of a second matrix beside the first (Operand::second), sixteen and
+// sixteen by turns, so that the two sums of a pair meet in one lane.
+template <int B, bool TR, int WAVES, int STAGES = TR ? 2 : 3, uint32_t UNIT = kSlab, bool ONCE = false, bool PAIRS = false>
 struct OperandStream {
+    static_assert(!PAIRS || TR, "columns are paired");
     static constexpr int kBytes = B * (int)UNIT * 2, I = kBytes / 1024 / WAVES;
     static constexpr int kStages = STAGES, kRing = kStages * kBytes;
     static constexpr int kHalf = I > 1 ? I / 2 : 1;
@@ -146,7 +150,10 @@ struct OperandStream {
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const uint32_t r = row_of(wave, i, lane), c = chunk_of(r, lane);
-            if (TR) {
+            if constexpr (PAIRS) {
+                const uint32_t column = 16u * (c >> 2) + 8u * (c & 1u);
+                off[i] = first + column < o.extent ? r * o.pitch + column * 2u + (c & 2u ? o.second : 0u) : kOutside;
+            } else if (TR) {
                 off[i] = r * o.pitch + (o.strip ? (c >> 4) * (uint32_t)(o.depth * 256u) + (c & 15u) * 16u : c * 16u);
                 if (first + 8u * c >= o.extent) off[i] = kOutside;
             } else {
@@ -227,12 +234,12 @@ struct Fragments {
 //   begin(Place, Held, m, n, lane): before the first multiply; (m, n) is the wavefront's corner in the tile;
 //   finish(Place, acc, Held, m, n, lane, landed): calls landed() before its first store.
 // Place has m0, n0 and depth.  The grid has at most tiles() workgroups.
-template <int BM, int BN, int WM, int WN, bool TRM, bool TRN>
+template <int BM, int BN, int WM, int WN, bool TRM, bool TRN, bool PAIRS = false>
 struct TileMfma {
     static constexpr int kWavesT = WM * WN, kThreads = 64 * kWavesT;
     static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;
     using SM = OperandStream<BM, TRM, kWavesT>;
-    using SN = OperandStream<BN, TRN, kWavesT>;
+    using SN = OperandStream<BN, TRN, kWavesT, TRN ? 2 : 3, kSlab, false, PAIRS>;
     static constexpr uint32_t kLds = SM::kRing + SN::kRing;
     static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
     static_assert(FM * FN > 1, "a k-step places its reads between its multiplies");
@@ -393,12 +400,12 @@ struct TileMfma {
 // requested into (second half of the next slab); after the other, its second half and the M slab (first half and M slab two
 // ahead).  Requests have the three k-steps to the barrier that needs them.
 // ONCE: the N side is requested non-temporally (weights that one row tile uses and that come from HBM).
-template <int BM, int BN, int WM, int WN, bool ONCE = false>
+template <int BM, int BN, int WM, int WN, bool ONCE = false, bool PAIRS = false>
 struct TilePair {
     static constexpr int kWavesT = WM * WN, kThreads = 64 * kWavesT;
     static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;
     using SM = OperandStream<BM, false, kWavesT, 2>;
-    using SN = OperandStream<BN, true, kWavesT, 3, kSlab / 2, ONCE>;
+    using SN = OperandStream<BN, true, kWavesT, 3, kSlab / 2, ONCE, PAIRS>;
     static constexpr uint32_t kLds = SM::kRing + SN::kRing;
     static_assert(kLds <= 80 * 1024, "half the LDS of a compute unit");
     typedef f32x16 Acc[FN][FM];
@@ -543,12 +550,12 @@ struct TilePair {
 // tiles keeps it full through the epilogues.  One barrier per slab: after it slab s has landed for everyone
 // and everyone has left the stage of slab s - 1, which is requested into at once.  HALVES: two sums per output, over the first and
 // over the second two k-steps of every slab, added at the end of a tile.
-template <int BM, int BN, int WM, int WN, bool TRN, int D, bool HALVES = false>
+template <int BM, int BN, int WM, int WN, bool TRN, int D, bool HALVES = false, bool PAIRS = false>
 struct TileStream {
     static constexpr int kWavesT = WM * WN, kThreads = 64 * kWavesT;
     static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;
     using SM = OperandStream<BM, false, kWavesT, D>;
-    using SN = OperandStream<BN, TRN, kWavesT, D>;
+    using SN = OperandStream<BN, TRN, kWavesT, D, kSlab, false, PAIRS>;
     static constexpr uint32_t kLds = SM::kRing + SN::kRing;
     static constexpr int kBehind = (D - 2) * (SM::I + SN::I);
     static_assert(kLds <= 160 * 1024 && kBehind <= 63, "LDS of a compute unit, largest count of s_waitcnt");

@@ -16,7 +16,8 @@ OK, QUEUED = 0, 1
 EINVAL, ENOMEM, ENOTRESIDENT, EBUSY, ENEVER, EHIP, ETIMEOUT = -1, -2, -3, -4, -5, -6, -7
 POLICY_FIFO, POLICY_FAIR, POLICY_PRIORITY, POLICY_PACK = 0, 1, 2, 3
 JOB_QUEUED, JOB_RESIDENT, JOB_EVICTED, JOB_DONE = 0, 1, 2, 3
-ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+ABSENT = 2 ** 64 - 1              # an offset that is not given
 F32, BF16 = 0, 1
 COPY_KERNEL, COPY_DMA = 0, 1
 LAYOUT_ROWMAJOR, LAYOUT_STRIP128 = 0, 1
@@ -69,6 +70,43 @@ class TrainDesc(C.Structure):
                 ("loss_off", C.c_uint64), ("work_off", C.c_uint64)]
 
 
+def _fields(head, offsets):
+    return head + [(name, C.c_uint64) for name in offsets.split()]
+
+
+_BLOCK = [("job", C.c_int32), ("M", C.c_uint32), ("K", C.c_uint32)]
+
+
+class GatedDesc(C.Structure):
+    _fields_ = _fields(_BLOCK + [("F", C.c_uint32), ("N", C.c_uint32), ("act", C.c_int32)],
+                       "w_in_off w_out_off x_off y_off h_off r_off gu_off")
+
+
+class GatedGradDesc(C.Structure):
+    _fields_ = _fields(_BLOCK + [("F", C.c_uint32), ("N", C.c_uint32), ("act", C.c_int32)],
+                       "w_in_off w_out_off x_off h_off gu_off dy_off dx_off dw_in_off dw_out_off work_off")
+
+
+class DenseDesc(C.Structure):
+    _fields_ = _fields(_BLOCK + [("N", C.c_uint32), ("act", C.c_int32), ("y_dtype", C.c_int32)],
+                       "w_off b_off x_off y_off r_off z_off")
+
+
+class DenseGradDesc(C.Structure):
+    _fields_ = _fields(_BLOCK + [("N", C.c_uint32), ("act", C.c_int32)],
+                       "w_off x_off z_off dy_off dx_off dw_off db_off work_off")
+
+
+class ClipTensor(C.Structure):
+    _fields_ = [("g_off", C.c_uint64), ("count", C.c_uint64), ("wm_off", C.c_uint64), ("wb_off", C.c_uint64),
+                ("dtype", C.c_int32), ("pad", C.c_int32)]
+
+
+class ClipDesc(C.Structure):
+    _fields_ = [("job", C.c_int32), ("n_tensors", C.c_uint32), ("tensors", C.POINTER(ClipTensor)),
+                ("max_norm", C.c_float), ("lr", C.c_float), ("norm_off", C.c_uint64), ("work_off", C.c_uint64)]
+
+
 class Stats(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in (
         "rounds", "iterations", "bytes_d2h", "bytes_h2d", "bytes_d2d", "moves", "compactions",
@@ -101,6 +139,15 @@ _PROTOS = {
     "salus_train_work_bytes": [C.c_uint32, C.POINTER(TrainLayer), C.c_uint32],
     "salus_forward_work_bytes": [C.c_uint32, C.POINTER(Layer), C.c_uint32, C.c_int32],
     "salus_grouped_train_step": [C.c_void_p, C.POINTER(TrainDesc), C.c_uint32, C.c_void_p],
+    "salus_grouped_gated_forward": [C.c_void_p, C.POINTER(GatedDesc), C.c_uint32, C.c_void_p],
+    "salus_grouped_gated_backward": [C.c_void_p, C.POINTER(GatedGradDesc), C.c_uint32, C.c_void_p],
+    "salus_gated_grad_work_bytes": [C.c_uint32, C.c_uint32],
+    "salus_grouped_dense_forward": [C.c_void_p, C.POINTER(DenseDesc), C.c_uint32, C.c_void_p],
+    "salus_grouped_dense_backward": [C.c_void_p, C.POINTER(DenseGradDesc), C.c_uint32, C.c_void_p],
+    "salus_dense_grad_work_bytes": [C.c_uint32, C.c_uint32],
+    "salus_grouped_clip": [C.c_void_p, C.POINTER(ClipDesc), C.c_uint32, C.c_void_p],
+    "salus_grouped_clip_sgd": [C.c_void_p, C.POINTER(ClipDesc), C.c_uint32, C.c_void_p],
+    "salus_clip_work_bytes": [C.POINTER(ClipTensor), C.c_uint32],
     "salus_switch_out": [C.c_void_p, C.c_int32, C.c_void_p],
     "salus_switch_in": [C.c_void_p, C.c_int32],
     "salus_switch_out_begin": [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p],
@@ -295,6 +342,71 @@ class Pool:
         return self._check(self._lib.salus_grouped_train_step(self._h, descs, n, stream),
                            (OK, EINVAL, ENOTRESIDENT, EBUSY))
 
+    # -- transformer blocks ----------------------------------------------------------
+    # make_*_descs: items are dicts with the C structure's fields; an offset that is left out is ABSENT.  They return
+    # (array, keepalive) ready for the call of the same name.
+    @staticmethod
+    def _make(kind, items):
+        items = list(items)
+        names = [name for name, _ in kind._fields_]
+        for it in items:
+            if not set(it) <= set(names):
+                raise ValueError(f"{kind.__name__} has no {sorted(set(it) - set(names))}")
+        return (kind * len(items))(*[kind(*[it.get(name, ABSENT) if name.endswith("_off") else it[name] for name in names])
+                                     for it in items]), []
+
+    @staticmethod
+    def make_gated_descs(items):
+        """dicts(job, M, K, F, N, act, w_in_off, w_out_off, x_off, y_off, h_off[, r_off][, gu_off])"""
+        return Pool._make(GatedDesc, items)
+
+    @staticmethod
+    def make_gated_grad_descs(items):
+        """dicts(job, M, K, F, N, act, w_in_off, w_out_off, x_off, h_off, gu_off, dy_off[, dx_off], dw_in_off, dw_out_off,
+        work_off)"""
+        return Pool._make(GatedGradDesc, items)
+
+    @staticmethod
+    def make_dense_descs(items):
+        """dicts(job, M, K, N, act, y_dtype, w_off[, b_off], x_off, y_off[, r_off][, z_off])"""
+        return Pool._make(DenseDesc, items)
+
+    @staticmethod
+    def make_dense_grad_descs(items):
+        """dicts(job, M, K, N, act, w_off, x_off[, z_off], dy_off[, dx_off], dw_off[, db_off], work_off)"""
+        return Pool._make(DenseGradDesc, items)
+
+    @staticmethod
+    def make_clip_descs(items):
+        """dicts(job, tensors=[dict(g_off, count, dtype[, wm_off, wb_off])], max_norm[, lr], norm_off, work_off)"""
+        items = list(items)
+        keep = [_clip_tensors(it["tensors"]) for it in items]
+        arr = (ClipDesc * len(items))(*[ClipDesc(it["job"], len(t), t, it["max_norm"], it.get("lr", 0.0), it["norm_off"], it["work_off"])
+                                        for it, t in zip(items, keep)])
+        return arr, keep
+
+    def _grouped(self, call, descs, n, stream):
+        return self._check(getattr(self._lib, call)(self._h, descs, len(descs) if n is None else n, stream),
+                           (OK, EINVAL, ENOTRESIDENT, EBUSY))
+
+    def grouped_gated_forward(self, descs, n=None, stream=None):
+        return self._grouped("salus_grouped_gated_forward", descs, n, stream)
+
+    def grouped_gated_backward(self, descs, n=None, stream=None):
+        return self._grouped("salus_grouped_gated_backward", descs, n, stream)
+
+    def grouped_dense_forward(self, descs, n=None, stream=None):
+        return self._grouped("salus_grouped_dense_forward", descs, n, stream)
+
+    def grouped_dense_backward(self, descs, n=None, stream=None):
+        return self._grouped("salus_grouped_dense_backward", descs, n, stream)
+
+    def grouped_clip(self, descs, n=None, stream=None):
+        return self._grouped("salus_grouped_clip", descs, n, stream)
+
+    def grouped_clip_sgd(self, descs, n=None, stream=None):
+        return self._grouped("salus_grouped_clip_sgd", descs, n, stream)
+
     # -- switching -----------------------------------------------------------------
     def switch_out(self, job, pinned_ptr=None):
         return self._lib.salus_switch_out(self._h, job, pinned_ptr)
@@ -343,6 +455,24 @@ def train_work_bytes(M, layers):
     """layers: [(K, N, wb_off, wm_off)]"""
     L = (TrainLayer * len(layers))(*[TrainLayer(*t) for t in layers])
     return lib().salus_train_work_bytes(M, L, len(layers))
+
+
+def gated_grad_work_bytes(M, F):
+    return lib().salus_gated_grad_work_bytes(M, F)
+
+
+def dense_grad_work_bytes(M, N):
+    return lib().salus_dense_grad_work_bytes(M, N)
+
+
+def _clip_tensors(tensors):
+    return (ClipTensor * len(tensors))(*[ClipTensor(t["g_off"], t["count"], t.get("wm_off", ABSENT), t.get("wb_off", ABSENT), t["dtype"])
+                                         for t in tensors])
+
+
+def clip_work_bytes(tensors):
+    """tensors: the dicts of make_clip_descs (only counts matter)"""
+    return lib().salus_clip_work_bytes(_clip_tensors(tensors), len(tensors))
 
 
 def scan_u64(values, scratch_ptr, stream=None):
