@@ -24,17 +24,41 @@ struct BlockArgs {
     BlockProblem p[kBlockProblems];
 };
 static_assert(sizeof(BlockArgs) <= 4096, "kernel arguments are limited to 4 KB");
+// The same for launches of few problems, whose time is the host's.
+constexpr uint32_t kBlockFew = 4;
+struct BlockFewArgs {
+    uint32_t n, tiles, pad[2];
+    uint32_t first[kBlockFew];
+    BlockProblem p[kBlockFew];
+};
 
 // What a product's sums become: Y = act(X W + B) + R; Y = act(X Wg) * (X Wu); [dG dU] of dH = X W^T; X W^T itself.
 enum class Epilogue { kDense, kGated, kGateGrad, kPlainT };
 
 // ---- activations ------------------------------------------------------------------------------------------------------------
-// NaNs pass through all of them, as they do through the products.  `fine`: for results that stay floats.  Rounded to bf16, whose half
-// step is 2^-9 of the value, the quick forms' 4e-7 (gelu_fast) and a few last bits (v_exp_f32, v_rcp_f32) do not show.
-__device__ inline float sigmoid_fast(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
-__device__ inline float sigmoid_fine(float z) { return 1.0f / (1.0f + expf(-z)); }
+// NaNs pass through all of them, as they do through the products.
+// Upper tail of the normal distribution at x >= 0: 2^p(x), p the polynomial of degree 8 that minimizes the largest x |2^p - Q| over [0, 6] (1e-8; fitted
+// by linear programming).  With it GELU(z) = z / 2 + |z| (1/2 - Q) is off by less than 8e-8 of |z| in float arithmetic (the library's erfc takes four
+// times as long: 24 jobs x 1 - 128 rows, 1000 -> 3080, float results, 9 of 49 us) and Phi by 1.3e-7, which is enough for results
+// that stay floats.  gelu_fast, two degrees less, suffices where a bf16 is next.
+__device__ inline float normal_tail(float x)
+{
+    const float c = fminf(x, 9.0f);
+    float p = fmaf(-1.8847762248697109e-06f, c, 2.7810900064650923e-05f);
+    p = fmaf(p, c, -0.00013004051288589835f);
+    p = fmaf(p, c, -0.0002765035897027701f);
+    p = fmaf(p, c, 0.007253301329910755f);
+    p = fmaf(p, c, -0.0526358038187027f);
+    p = fmaf(p, c, -0.4591573178768158f);
+    p = fmaf(p, c, -1.15111243724823f);
+    p = fmaf(p, c, -0.9999998211860657f);
+    return __builtin_amdgcn_exp2f(p);
+}
+// exp's argument is off by 2^-24 of itself, which the slope of the sigmoid takes back: 3e-8 of |z| at most in z sigmoid(z), beside the last bits of v_exp_f32 and v_rcp_f32.
+__device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
 __device__ inline float relu_nan(float z) { return z < 0.0f ? 0.0f : z; }
 
+// `fine`: for results that stay floats.
 template <int N>
 __device__ inline void activate_all(float (&z)[N], uint32_t act, bool fine)
 {
@@ -43,23 +67,17 @@ __device__ inline void activate_all(float (&z)[N], uint32_t act, bool fine)
         for (int i = 0; i < N; ++i) z[i] = relu_nan(z[i]);
     } else if (act == 2 && fine) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = 0.5f * z[i] * erfcf(-0.70710678118654752440f * z[i]);
+        for (int i = 0; i < N; ++i) z[i] = fmaf(fabsf(z[i]), 0.5f - normal_tail(fabsf(z[i])), 0.5f * z[i]);
     } else if (act == 2) {
 #pragma unroll
         for (int i = 0; i < N; ++i) z[i] = gelu_fast(z[i]);
-    } else if (act == 3 && fine) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = z[i] * sigmoid_fine(z[i]);
     } else if (act == 3) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = z[i] * sigmoid_fast(z[i]);
+        for (int i = 0; i < N; ++i) z[i] = z[i] * sigmoid(z[i]);
     }
 }
 
-// GELU'(z) = Phi(z) + z phi(z), SiLU'(z) = s (1 + z (1 - s)), s = 1 / (1 + exp -z).
-constexpr float kInvSqrt2Pi = 0.39894228040143267794f;
-
-// a = act(z), d = act'(z); a factor for results that are rounded to bf16.
+// a = act(z), d = act'(z): GELU'(z) = Phi(z) + z phi(z), SiLU'(z) = s (1 + z (1 - s)), s = sigmoid(z).
 template <int N>
 __device__ inline void activate_with_slope(const float (&z)[N], float (&a)[N], float (&d)[N], uint32_t act)
 {
@@ -72,15 +90,15 @@ __device__ inline void activate_with_slope(const float (&z)[N], float (&a)[N], f
     } else if (act == 2) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            a[i] = gelu_fast(z[i]);
-            // Phi = a / z, whose error is at most 64 times the activation's, 2.6e-5; for |z| < 1 / 64 the first terms of its series (2.5e-7)
-            const float phi = kInvSqrt2Pi * __builtin_amdgcn_exp2f(-0.72134752f * z[i] * z[i]);
-            d[i] = fmaf(z[i], phi, fabsf(z[i]) < 0.015625f ? fmaf(z[i], kInvSqrt2Pi, 0.5f) : a[i] * __builtin_amdgcn_rcpf(z[i]));
+            const float x = fabsf(z[i]), q = normal_tail(x);
+            const float phi = 0.39894228040143267794f * __builtin_amdgcn_exp2f(-0.72134752f * z[i] * z[i]);
+            a[i] = fmaf(x, 0.5f - q, 0.5f * z[i]);
+            d[i] = fmaf(z[i], phi, z[i] < 0.0f ? q : 1.0f - q);
         }
     } else if (act == 3) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float s = sigmoid_fast(z[i]);
+            const float s = sigmoid(z[i]);
             a[i] = z[i] * s;
             d[i] = s * fmaf(z[i], 1.0f - s, 1.0f);
         }
@@ -91,18 +109,6 @@ __device__ inline void activate_with_slope(const float (&z)[N], float (&a)[N], f
             d[i] = 1.0f;
         }
     }
-}
-
-// The slope alone, to the last bits (its sums stay floats).
-__device__ inline float slope_fine(float z, uint32_t act)
-{
-    if (act == 1) return z > 0.0f ? 1.0f : 0.0f;
-    if (act == 2) return fmaf(z, kInvSqrt2Pi * expf(-0.5f * z * z), 0.5f * erfcf(-0.70710678118654752440f * z));
-    if (act == 3) {
-        const float s = sigmoid_fine(z);
-        return s * fmaf(z, 1.0f - s, 1.0f);
-    }
-    return 1.0f;
 }
 
 // ---- sums on their way to memory ----------------------------------------------------------------------------------------------
@@ -159,8 +165,8 @@ __device__ inline void store_bf16(uint16_t *Y, uint32_t pitch, const Part &at, u
 }
 
 // act(sums + B) + R; the sums with B to Z.  N is a multiple of 8, so a vector of up to 8 columns lies wholly inside or outside.
-// Everything that is read is asked for before the activations and used behind them.
-template <int J>
+// EARLY: R is asked for before the activations and used behind them, where there are registers for that.
+template <int J, bool EARLY>
 __device__ inline void finish_dense(const BlockProblem &p, const Part &at, uint32_t r0, uint32_t c0, const float (&v)[J][16], int lane)
 {
     const uint32_t N = p.N, act = p.flags & 0xffu, column = line_column_f32(lane);
@@ -169,7 +175,8 @@ __device__ inline void finish_dense(const BlockProblem &p, const Part &at, uint3
     const uint16_t *R = (const uint16_t *)p.R + corner;
     uint32_t wide[4][4];
     u32x2 narrow[J][4];
-    if (p.R) {
+    auto ask_residual = [&]() {
+        if (!p.R) return;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const uint32_t r = r0 + 8u * q + (lane & 7);
@@ -186,7 +193,8 @@ __device__ inline void finish_dense(const BlockProblem &p, const Part &at, uint3
                 }
             }
         }
-    }
+    };
+    if (EARLY) ask_residual();
     Lines o[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
@@ -211,6 +219,7 @@ __device__ inline void finish_dense(const BlockProblem &p, const Part &at, uint3
         }
         activate_all(*(float (*)[16])&o[j], act, !out_bf16);
     }
+    if (!EARLY) ask_residual();
     if (p.R) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -274,42 +283,62 @@ __device__ inline void finish_gated(const BlockProblem &p, const Part &at, uint3
     store_bf16<J>((uint16_t *)p.Y + (uint64_t)at.m * N + at.n, N, at, r0, c0, h, lane);
 }
 
-// dG = dH * u * act'(g) and dU = dH * act(g), beside each other, of J blocks of dH.
+// dG = dH * u * act'(g) and dU = dH * act(g), beside each other, of J blocks of dH.  Eight rows at a time, the next eight asked for
+// meanwhile: more of g and u does not fit beside the sums of a large tile.
 template <int J>
 __device__ inline void finish_gate_grad(const BlockProblem &p, const Part &at, uint32_t r0, uint32_t c0, const float (&v)[J][16], int lane)
 {
     const uint32_t N = p.N, column = line_column_f32(lane);
-    Lines dg[J], du[J];
+    const float *Z = p.Z + (uint64_t)at.m * (2 * N) + at.n;
+    uint16_t *Y = (uint16_t *)p.Y + (uint64_t)at.m * (2 * N) + at.n;
+    f32x4 g[2][J], u[2][J];
+    auto load = [&](int q) {
+        const uint32_t r = r0 + 8u * q + (lane & 7);
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-        Lines dh, g, u;
-        const uint32_t c = c0 + 32u * j + column;
-        const float *Z = p.Z + (uint64_t)at.m * (2 * N) + at.n + c;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint32_t r = r0 + 8u * q + (lane & 7);
+        for (int j = 0; j < J; ++j) {
+            const uint32_t c = c0 + 32u * j + column;
             const bool in = r < at.rows && c < at.cols;
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            const f32x4 gv = in ? *(const f32x4 *)(Z + (size_t)r * (2 * N)) : zero, uv = in ? *(const f32x4 *)(Z + (size_t)r * (2 * N) + N) : zero;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                g[q][e] = gv[e];
-                u[q][e] = uv[e];
-            }
+            g[q & 1][j] = in ? *(const f32x4 *)(Z + (size_t)r * (2 * N) + c) : zero;
+            u[q & 1][j] = in ? *(const f32x4 *)(Z + (size_t)r * (2 * N) + N + c) : zero;
         }
-        to_lines(v[j], dh);
-        activate_with_slope(*(const float (*)[16])&g, *(float (*)[16])&du[j], *(float (*)[16])&dg[j], p.flags & 0xffu);
+    };
+    load(0);
+    Lines dh[J];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+    for (int j = 0; j < J; ++j) to_lines(v[j], dh[j]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (q < 3) load(q + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        float z[4 * J], du[J][4], dg[J][4];
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[4 * j + e] = g[q & 1][j][e];
+        activate_with_slope(z, *(float (*)[4 * J])&du, *(float (*)[4 * J])&dg, p.flags & 0xffu);
+#pragma unroll
+        for (int j = 0; j < J; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                du[j][q][e] *= dh[q][e];
-                dg[j][q][e] *= dh[q][e] * u[q][e];
+                du[j][e] *= dh[j][q][e];
+                dg[j][e] *= dh[j][q][e] * u[q & 1][j][e];
             }
+        const uint32_t r = r0 + 8u * q + (lane & 7), c = c0 + (J == 2 ? pair_column(lane) : column);
+        const bool in = r < at.rows && c < at.cols;
+        uint16_t *to = Y + (size_t)r * (2 * N) + c;
+        if constexpr (J == 2) {
+            const u32x4 wg = pair_up(dg[0], dg[1]), wu = pair_up(du[0], du[1]);
+            if (in) {
+                *(u32x4 *)to = wg;
+                *(u32x4 *)(to + N) = wu;
+            }
+        } else if (in) {
+            *(u32x2 *)to = u32x2{bf16_pack(dg[0][0], dg[0][1]), bf16_pack(dg[0][2], dg[0][3])};
+            *(u32x2 *)(to + N) = u32x2{bf16_pack(du[0][0], du[0][1]), bf16_pack(du[0][2], du[0][3])};
+        }
+        __builtin_amdgcn_sched_barrier(0);
     }
-    uint16_t *Y = (uint16_t *)p.Y + (uint64_t)at.m * (2 * N) + at.n;
-    store_bf16<J>(Y, 2 * N, at, r0, c0, dg, lane);
-    store_bf16<J>(Y + N, 2 * N, at, r0, c0, du, lane);
 }
 
 // ---- tile walks (tile_mfma.hpp) ---------------------------------------------------------------------------------------------------
@@ -388,7 +417,7 @@ struct BlockWalk {
                         for (int jj = 0; jj < J; ++jj) to_lines(v[jj], o[jj]);
                         store_bf16<J>((uint16_t *)p.Y + (uint64_t)at.m * p.N + at.n, p.N, at, 32u * i, 32u * j, o, lane);
                     } else {
-                        finish_dense<J>(p, at, 32u * i, 32u * j, v, lane);
+                        finish_dense<J, FM * FN <= 4>(p, at, 32u * i, 32u * j, v, lane);
                     }
                 }
             }

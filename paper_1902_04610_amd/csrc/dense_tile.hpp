@@ -9,10 +9,16 @@ namespace salus {
 // of every 16x16 block holds row 4*(lane/16)+r, so wavefront w ends up owning
 // rows with r == w: each wavefront sends the other three quarters through LDS
 // and adds what it receives in a fixed order.
+constexpr int sums_per_pass(int n)
+{
+    int g = n < 16 ? n : 16;
+    while (n % g != 0) --g;
+    return g;
+}
 template <int NACC>
 __device__ inline void reduce_scatter(f32x4 (&acc)[NACC], float (&own)[NACC], float *lds)
 {
-    constexpr int G = NACC < 16 ? NACC : 16;    // accumulators per pass (bounds the LDS footprint)
+    constexpr int G = sums_per_pass(NACC);      // accumulators per pass (bounds the LDS footprint)
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // lds[dst wave][source slot][accumulator in pass][lane]
@@ -42,7 +48,7 @@ __device__ inline void reduce_scatter(f32x4 (&acc)[NACC], float (&own)[NACC], fl
 }
 
 template <int NACC>
-constexpr int reduce_lds_floats() { return kWaves * 3 * (NACC < 16 ? NACC : 16) * 64; }
+constexpr int reduce_lds_floats() { return kWaves * 3 * sums_per_pass(NACC) * 64; }
 
 // ---------------------------------------------------------------------------
 // bf16 weights and activations, float accumulation, v_mfma_f32_16x16x32_bf16.
@@ -63,8 +69,10 @@ constexpr int reduce_lds_floats() { return kWaves * 3 * (NACC < 16 ? NACC : 16) 
 // CPL: columns per lane, 8, 4 or 2; the tile is 16 * CPL columns wide.  An output's products are summed in the same order
 // whatever the width, so the result is the same to the bit.  D: k-steps in flight per wavefront; a narrow tile has fewer
 // bytes per step and needs more of them to cover the latency.
-template <int MT, bool TW, bool NT, int CPL = 8, int D = 2>
-__device__ inline void dense_bf16_tile(const Problem &p, const Tile tile, float *lds)
+// The sums alone (of a Problem, or of anything with its W, X, M, K, N and flags): own[t * CPL + i] is row m0 + 16 t + 4 (lane / 16) + wave, column n0 +
+// CPL * (lane % 16) + i.
+template <int MT, bool TW, bool NT, int CPL, int D, typename P>
+__device__ inline void dense_bf16_sums(const P &p, const Tile tile, float *lds, float (&own)[MT * CPL])
 {
     constexpr int NACC = MT * CPL, NROW = TW ? CPL : 8;      // weight vectors per lane and k-step
     typedef unsigned int wvec __attribute__((ext_vector_type(TW ? 4 : CPL / 2)));
@@ -205,9 +213,20 @@ __device__ inline void dense_bf16_tile(const Problem &p, const Tile tile, float 
             if (d + D < left) compute(w[d], x[d], ok[d]);
     }
 
-    float own[NACC];
     reduce_scatter<NACC>(acc, own, lds);
+}
 
+template <int MT, bool TW, bool NT, int CPL = 8, int D = 2>
+__device__ inline void dense_bf16_tile(const Problem &p, const Tile tile, float *lds)
+{
+    float own[MT * CPL];
+    dense_bf16_sums<MT, TW, NT, CPL, D>(p, tile, lds, own);
+
+    const uint32_t M = p.M, N = p.N, xtiles = (M + 15) / 16;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t ncol = tile.n0 + CPL * c;
+    const bool col_ok = ncol < N;
     const uint32_t act = p.flags & 0xffu;
 #pragma unroll
     for (int t = 0; t < MT; ++t) {

@@ -3,35 +3,179 @@
 // the product of the halves, the residual, the gate's derivative) happens on its float sums on the way to memory (block.hpp), so that
 // a round of dense layers is one launch and one of gated blocks is two.
 #include <algorithm>
+#include <type_traits>
+#include <vector>
 
 #include "block.hpp"
+#include "narrow_tile.hpp"
 
 namespace salus {
 
 // 64-row tiles, operands through an LDS ring (TileStream), two workgroups per compute unit.  Right for every size: rows and columns outside
 // are neither fetched nor stored.
-template <int BM, int BN, int WM, int WN, int D, Epilogue E>
-__global__ __launch_bounds__(64 * WM * WN, 2) void block_stream(BlockArgs a)
+template <int BM, int BN, int WM, int WN, int D, Epilogue E, bool ONCE = false>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN / 2) void block_stream(BlockArgs a)
 {
     using Walk = BlockWalk<BM, BN, E>;
-    using T = TileStream<BM, BN, WM, WN, !Walk::kTransposed, D, false, E == Epilogue::kGated>;
+    using T = TileStream<BM, BN, WM, WN, !Walk::kTransposed, D, false, E == Epilogue::kGated, ONCE>;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[T::kLds];
     const Walk walk(a);
     T::run(walk, smem);
 }
 
-template <int BM, int COLS>
-static hipError_t launch_block(void (*kernel)(BlockArgs), int threads, uint32_t per_cu, const BlockProblem *p, uint32_t n, hipStream_t stream,
-                               uint64_t *launches)
+// Large tiles (TileMfma, TilePair, TileRows): where a weight is used by 128 rows and more, or comes in whole rounds of tiles.
+template <int BM, int BN, int WM, int WN, Epilogue E, bool ONCE = false>
+__global__ __launch_bounds__(64 * WM * WN, 2) void block_tiled(BlockArgs a)
 {
-    for (uint32_t at = 0; at < n; at += kBlockProblems) {
-        BlockArgs a{};
-        const uint64_t tiles = fill_group(a, p + at, std::min(kBlockProblems, n - at),
-                                          [](const BlockProblem &q) { return (uint64_t)((q.M + BM - 1) / BM) * ((q.N + COLS - 1) / COLS); });
+    using Walk = BlockWalk<BM, BN, E>;
+    constexpr bool kPairs = E == Epilogue::kGated;
+    using T = std::conditional_t<Walk::kTransposed, TileRows<BM, BN, WM, WN>,
+                                 std::conditional_t<BM * BN == 128 * 256, TilePair<BM, BN, WM, WN, ONCE, kPairs>, TileMfma<BM, BN, WM, WN, false, true, kPairs>>>;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[T::kLds];
+    const Walk walk(a);
+    T::run(walk, smem);
+}
+
+// Few rows (at most 16 MT): tiles of 16 NB columns of weights, K split over the four wavefronts of a workgroup, weights straight into an LDS ring per
+// wavefront (NarrowTile).  Gated: half the columns are the gate's.  TWO: two workgroups per compute unit.
+template <int MT, int NB, bool TWO, bool GATED, typename Args>
+__device__ inline void narrow_block(const Args &a, unsigned char *smem)
+{
+    using T = std::conditional_t<TWO, NarrowTile<MT, NB, 1, 80 * 1024>, NarrowTile<MT, NB>>;
+    constexpr uint32_t kCols = GATED ? 8 * NB : 16 * NB;
+    BlockProblem p;
+    const uint32_t t = find_owner(a.first, a.p, xcd_remap(blockIdx.x, a.tiles), p);
+    const uint32_t M = p.M, N = p.N, act = p.flags & 0xffu, rt = (M + 16 * MT - 1) / (16 * MT);
+    const Tile tile = {t % rt * 16 * MT, t / rt * kCols};      // row tiles of one column tile are neighbours: they share W
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    auto row_of = [&](int i) { return tile.m0 + 16u * i + 4u * g + wave; };
+    float own[MT * NB];
+    if constexpr (GATED) {
+        T::template sums<true, true>(p.W, p.X, M, p.K, N, false, false, N * 4u, N * 2u, tile, smem, own);
+        constexpr int H = NB / 2;
+        float h[MT * H];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                const uint32_t row = row_of(i), n = tile.n0 + 16 * j + c;
+                const float gate = own[i * NB + j];
+                if (p.Z && row < M && n < N) {
+                    Global<float> *Z = (Global<float> *)p.Z + (size_t)row * (2 * N) + n;
+                    Z[0] = gate;
+                    Z[N] = own[i * NB + H + j];
+                }
+                h[i * H + j] = gate;
+            }
+        activate_all(h, act, false);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                const uint32_t row = row_of(i), n = tile.n0 + 16 * j + c;
+                if (row < M && n < N) ((Global<uint16_t> *)p.Y)[(size_t)row * N + n] = (uint16_t)bf16_bits(h[i * H + j] * own[i * NB + H + j]);
+            }
+    } else {
+        // bias and residual are asked for in front of everything else
+        uint16_t r[MT * NB] = {}, b[NB] = {};
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const uint32_t n = tile.n0 + 16 * j + c;
+            if (p.B && n < N) b[j] = ((const Global<uint16_t> *)p.B)[n];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                if (p.R && row_of(i) < M && n < N) r[i * NB + j] = ((const Global<uint16_t> *)p.R)[(size_t)row_of(i) * N + n];
+        }
+        T::template sums<false, true>(p.W, p.X, M, p.K, N, false, false, N * 2u, 0, tile, smem, own);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                const uint32_t row = row_of(i), n = tile.n0 + 16 * j + c;
+                own[i * NB + j] += bf16_low(b[j]);
+                if (p.Z && row < M && n < N) ((Global<float> *)p.Z)[(size_t)row * N + n] = own[i * NB + j];
+            }
+        const bool out_bf16 = (p.flags & kOutBf16) != 0;
+        activate_all(own, act, !out_bf16);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                const uint32_t row = row_of(i), n = tile.n0 + 16 * j + c;
+                if (row >= M || n >= N) continue;
+                const float v = own[i * NB + j] + bf16_low(r[i * NB + j]);
+                if (out_bf16) ((Global<uint16_t> *)p.Y)[(size_t)row * N + n] = (uint16_t)bf16_bits(v);
+                else ((Global<float> *)p.Y)[(size_t)row * N + n] = v;
+            }
+    }
+}
+template <int MT, int NB, bool TWO, bool GATED, typename Args>
+__global__ __launch_bounds__(kGemmThreads, TWO ? 2 : 1) void block_narrow(Args a)
+{
+    using T = std::conditional_t<TWO, NarrowTile<MT, NB, 1, 80 * 1024>, NarrowTile<MT, NB>>;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[T::kLds];
+    narrow_block<MT, NB, TWO, GATED>(a, smem);
+}
+
+// The gate's derivative for few rows or few tiles: 16 CPL columns, K split over the four wavefronts, weights through registers, whose lanes load 16 bytes along
+// a transposed weight's rows as it is (dense_bf16_sums).  Deep layers keep eight or four k-steps in flight instead of two.
+template <int MT, int CPL, int D>
+__device__ inline void narrow_gate_grad(const BlockProblem &p, const Tile tile, float *lds)
+{
+    float own[MT * CPL];
+    dense_bf16_sums<MT, true, false, CPL, D>(p, tile, lds, own);
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t N = p.N, n = tile.n0 + CPL * c;
+    typedef float vec __attribute__((ext_vector_type(CPL)));
+    typedef uint32_t out_vec __attribute__((ext_vector_type(CPL / 2)));
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const uint32_t row = tile.m0 + 16 * t + 4 * g + wave;
+        if (row >= p.M || n >= N) continue;
+        const Global<float> *Z = (const Global<float> *)p.Z + (size_t)row * (2 * N) + n;
+        const vec gate = *(const Global<vec> *)Z, up = *(const Global<vec> *)(Z + N);
+        float z[CPL], du[CPL], dg[CPL];
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) z[i] = gate[i];
+        activate_with_slope(z, du, dg, p.flags & 0xffu);
+        out_vec og, ou;
+#pragma unroll
+        for (int i = 0; i < CPL; i += 2) {
+            og[i / 2] = bf16_pack(own[t * CPL + i] * up[i] * dg[i], own[t * CPL + i + 1] * up[i + 1] * dg[i + 1]);
+            ou[i / 2] = bf16_pack(own[t * CPL + i] * du[i], own[t * CPL + i + 1] * du[i + 1]);
+        }
+        Global<uint16_t> *Y = (Global<uint16_t> *)p.Y + (size_t)row * (2 * N) + n;
+        *(Global<out_vec> *)Y = og;
+        *(Global<out_vec> *)(Y + N) = ou;
+    }
+}
+constexpr uint32_t kGateDeepK = 2048;
+template <int MT, int CPL, typename Args>
+__global__ __launch_bounds__(kGemmThreads) void block_gate_grad_narrow(Args a)
+{
+    __shared__ float lds[reduce_lds_floats<MT * CPL>()];
+    BlockProblem p;
+    const uint32_t t = find_owner(a.first, a.p, xcd_remap(blockIdx.x, a.tiles), p), rt = (p.M + 16 * MT - 1) / (16 * MT);
+    const Tile tile = {t % rt * 16 * MT, t / rt * 16 * CPL};
+    if (p.K > kGateDeepK) narrow_gate_grad<MT, CPL, 16 / CPL>(p, tile, lds);
+    else narrow_gate_grad<MT, CPL, 2>(p, tile, lds);
+}
+
+// Launches of at most as many problems as Args holds: bm rows and `cols` output columns a tile, at most `grid` workgroups (0: one per tile).
+template <typename Args>
+static hipError_t launch_block(void (*kernel)(Args), int threads, uint32_t bm, uint32_t cols, uint32_t grid, const BlockProblem *p, uint32_t n,
+                               hipStream_t stream, uint64_t *launches)
+{
+    constexpr uint32_t kMost = sizeof(Args::first) / 4;
+    for (uint32_t at = 0; at < n; at += kMost) {
+        Args a{};
+        const uint64_t tiles = fill_group(a, p + at, std::min(kMost, n - at),
+                                          [&](const BlockProblem &q) { return (uint64_t)((q.M + bm - 1) / bm) * ((q.N + cols - 1) / cols); });
         if (tiles == 0) continue;
         if (tiles > 0x7fffffffull) return hipErrorInvalidValue;
-        const uint32_t grid = (uint32_t)std::min<uint64_t>(tiles, resident_grid() * per_cu);
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, stream, a);
+        hipLaunchKernelGGL(kernel, dim3(grid ? (uint32_t)std::min<uint64_t>(tiles, grid) : (uint32_t)tiles), dim3(threads), 0, stream, a);
         if (launches) *launches += 1;
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -39,76 +183,243 @@ static hipError_t launch_block(void (*kernel)(BlockArgs), int threads, uint32_t 
     return hipSuccess;
 }
 
+struct Round {
+    const BlockProblem *p;
+    uint32_t n;
+    hipStream_t stream;
+    uint64_t *launches;
+};
+
+// One way to run a round: tiles of bm rows and `cols` columns of the output, per_cu of them at a time on a compute unit, for rounds whose largest job has
+// more than `above` and at most `upto` rows; how long a launch takes in nanoseconds: fixed + rounds of tiles x (slabs of 64 of the depth x slab + rest).
+struct Tiling {
+    uint32_t bm, cols, per_cu, above, upto, fixed, slab, rest;
+    hipError_t (*launch)(const Round &);
+};
+constexpr uint32_t kAnyRows = ~0u;
+
+static uint64_t launch_ns(const Tiling &t, const BlockProblem *p, uint32_t n)
+{
+    uint64_t tiles = 0, work = 0;
+    for (uint32_t i = 0; i < n; ++i) {
+        const uint64_t count = (uint64_t)((p[i].M + t.bm - 1) / t.bm) * ((p[i].N + t.cols - 1) / t.cols);
+        tiles += count;
+        work += count * ((uint64_t)std::max((p[i].K + kSlab - 1) / kSlab, kMinSlabs) * t.slab + t.rest);
+    }
+    if (tiles == 0) return 0;
+    // a last round that leaves half of the compute units one tile instead of two takes 0.6 of the time of a full one
+    const uint64_t cus = resident_grid(), grid = cus * t.per_cu, last = tiles % grid;
+    const uint64_t tenths = tiles / grid * 10 + (last == 0 ? 0 : t.per_cu == 1 || last > cus ? 10 : 6);
+    return t.fixed + tenths * (work / tiles) / 10;
+}
+
+struct Choice { const Tiling *tiling; uint64_t ns; };
+template <size_t N>
+static Choice choose(const Tiling (&tilings)[N], const BlockProblem *p, uint32_t n)
+{
+    uint32_t rows = 0;
+    for (uint32_t i = 0; i < n; ++i) rows = std::max(rows, p[i].M);
+    Choice best{nullptr, ~0ull};
+    for (const Tiling &t : tilings) {
+        if (rows <= t.above || rows > t.upto) continue;
+        const uint64_t ns = launch_ns(t, p, n);
+        if (ns < best.ns) best = {&t, ns};
+    }
+    return best;
+}
+
+template <int MT, int NB, bool TWO, Epilogue E>
+static hipError_t narrow(const Round &r)
+{
+    constexpr bool kGated = E == Epilogue::kGated;
+    constexpr uint32_t kCols = kGated ? 8 * NB : 16 * NB;
+    if (r.n <= kBlockFew) return launch_block<BlockFewArgs>(block_narrow<MT, NB, TWO, kGated, BlockFewArgs>, kGemmThreads, 16 * MT, kCols, 0, r.p, r.n, r.stream, r.launches);
+    return launch_block<BlockArgs>(block_narrow<MT, NB, TWO, kGated, BlockArgs>, kGemmThreads, 16 * MT, kCols, 0, r.p, r.n, r.stream, r.launches);
+}
+template <int MT, int CPL>
+static hipError_t narrow_grad(const Round &r)
+{
+    if (r.n <= kBlockFew) return launch_block<BlockFewArgs>(block_gate_grad_narrow<MT, CPL, BlockFewArgs>, kGemmThreads, 16 * MT, 16 * CPL, 0, r.p, r.n, r.stream, r.launches);
+    return launch_block<BlockArgs>(block_gate_grad_narrow<MT, CPL, BlockArgs>, kGemmThreads, 16 * MT, 16 * CPL, 0, r.p, r.n, r.stream, r.launches);
+}
+template <int BM, int BN, int WM, int WN, int D, Epilogue E>
+static hipError_t ring(const Round &r)
+{
+    return launch_block<BlockArgs>(block_stream<BM, BN, WM, WN, D, E>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, 2 * resident_grid(), r.p, r.n, r.stream, r.launches);
+}
+template <int BM, int BN, int WM, int WN, int PER_CU, Epilogue E>
+static hipError_t tiled(const Round &r)
+{
+    return launch_block<BlockArgs>(block_tiled<BM, BN, WM, WN, E>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, PER_CU * resident_grid(), r.p, r.n, r.stream, r.launches);
+}
+
+// Fitted to launches of drawn sizes (1 - 48 jobs of 1 - 4096 rows, widths of 64 - 8192; 210 dense, 105 gated, 61 gate gradients, 100 input gradients, kernel
+// traces of every kind of tile on each of them): off by 6 - 10 % in the median.  The choice is 1.9 % (dense), 2.7 % (gated) and 1.9 % (gate gradients) off the quickest kind on
+// average and 28, 33 and 34 % at most; the best single kind is 38 (64 x 64), 32 (64 x 128) and 25 % (32 x 32) off.  What each is for: narrow tiles fill the chip with few rows, the
+// ring streams weights past one or two row tiles, large tiles multiply.  1 job x 1 row, 4096 -> 1024: 16 columns 9.4 us, the ring 16; 32 jobs x 1 - 32 rows, 1000 -> 5520, 64 x 64 / 128 x 128 / 128 x 256
+// 75 / 73 / 73, 2760 -> 1000 37 / 37 / 55; 8 jobs x 64 rows, 2736 -> 1024, 32 x 64 / 64 x 64 20.7 / 25.8; 8 jobs x 1000 rows, 2048 -> 8192, 64 x 128 / 128 x 128 / 128 x 256 / 256 x 256 545 / 353 / 295 / 286.
+constexpr Tiling kDense[] = {
+    {16, 16, 1, 0, 16, 1300, 92, 1370, narrow<1, 1, false, Epilogue::kDense>},
+    {32, 16, 1, 16, kAnyRows, 1300, 152, 1480, narrow<2, 1, false, Epilogue::kDense>},
+    {16, 32, 1, 0, 16, 1100, 109, 1870, narrow<1, 2, false, Epilogue::kDense>},
+    {32, 32, 1, 16, kAnyRows, 1100, 178, 2140, narrow<2, 2, false, Epilogue::kDense>},
+    {16, 64, 2, 0, 16, 1400, 243, 3080, narrow<1, 4, true, Epilogue::kDense>},
+    {32, 64, 2, 16, kAnyRows, 1800, 378, 3280, narrow<2, 4, true, Epilogue::kDense>},
+    {64, 64, 2, 0, kAnyRows, 2400, 471, 2510, ring<64, 64, 2, 2, 4, Epilogue::kDense>},
+    {128, 128, 2, 0, kAnyRows, 2900, 923, 6250, tiled<128, 128, 2, 2, 2, Epilogue::kDense>},
+    {128, 256, 2, 0, kAnyRows, 2900, 1439, 10780, tiled<128, 256, 1, 4, 2, Epilogue::kDense>},
+    {256, 256, 1, 0, kAnyRows, 0, 1180, 11130, tiled<256, 256, 2, 4, 1, Epilogue::kDense>},
+};
+constexpr Tiling kGated[] = {      // half of a tile's columns are the gate's
+    {16, 16, 1, 0, 16, 1100, 166, 1560, narrow<1, 2, false, Epilogue::kGated>},
+    {32, 16, 1, 16, kAnyRows, 1700, 248, 1110, narrow<2, 2, false, Epilogue::kGated>},
+    {16, 32, 2, 0, 16, 1400, 341, 2450, narrow<1, 4, true, Epilogue::kGated>},
+    {32, 32, 2, 16, kAnyRows, 2300, 499, 1040, narrow<2, 4, true, Epilogue::kGated>},
+    {64, 64, 2, 0, kAnyRows, 2400, 806, 2280, ring<64, 128, 2, 2, 3, Epilogue::kGated>},
+    {128, 64, 2, 0, kAnyRows, 2400, 1036, 3920, tiled<128, 128, 2, 2, 2, Epilogue::kGated>},
+    {128, 128, 2, 0, kAnyRows, 1400, 1471, 8870, tiled<128, 256, 1, 4, 2, Epilogue::kGated>},
+    {256, 128, 1, 0, kAnyRows, 800, 1259, 8090, tiled<256, 256, 2, 4, 1, Epilogue::kGated>},
+};
+constexpr Tiling kGateGrad[] = {
+    {16, 32, 1, 0, 16, 2800, 121, 230, narrow_grad<1, 2>},
+    {32, 32, 1, 16, kAnyRows, 2500, 165, 830, narrow_grad<2, 2>},
+    {16, 64, 1, 0, 16, 3000, 209, 270, narrow_grad<1, 4>},
+    {32, 64, 1, 16, kAnyRows, 2700, 269, 1120, narrow_grad<2, 4>},
+    {64, 64, 2, 0, kAnyRows, 2000, 442, 4720, ring<64, 64, 2, 2, 4, Epilogue::kGateGrad>},
+    {64, 128, 2, 0, kAnyRows, 800, 627, 8500, ring<64, 128, 2, 2, 3, Epilogue::kGateGrad>},
+    {128, 128, 2, 0, kAnyRows, 0, 904, 14890, tiled<128, 128, 2, 2, 2, Epilogue::kGateGrad>},
+    {256, 256, 1, 0, kAnyRows, 0, 1074, 19050, tiled<256, 256, 2, 4, 1, Epilogue::kGateGrad>},
+};
+// Input gradients: large tiles, if they are quicker than what the grouped dense layers have for transposed weights (launch_grouped_bf16), for which the ring's
+// tiles stand here.
+constexpr Tiling kInputLarge[] = {
+    {128, 128, 2, 0, kAnyRows, 1400, 886, 3750, tiled<128, 128, 2, 2, 2, Epilogue::kPlainT>},
+    {256, 256, 1, 0, kAnyRows, 0, 1033, 6770, tiled<256, 256, 2, 4, 1, Epilogue::kPlainT>},
+};
+constexpr Tiling kInputRing[] = {
+    {64, 64, 2, 0, kAnyRows, 2100, 405, 1920, nullptr},
+    {64, 128, 2, 0, kAnyRows, 1400, 605, 2940, nullptr},
+};
+
 hipError_t launch_block_dense(const BlockProblem *p, uint32_t n, bool, hipStream_t stream, uint64_t *launches)
 {
-    return launch_block<64, 128>(block_stream<64, 128, 2, 2, 3, Epilogue::kDense>, 256, 2, p, n, stream, launches);
+    return choose(kDense, p, n).tiling->launch({p, n, stream, launches});
 }
 
 hipError_t launch_block_gated(const BlockProblem *p, uint32_t n, bool, hipStream_t stream, uint64_t *launches)
 {
-    return launch_block<64, 64>(block_stream<64, 128, 2, 2, 3, Epilogue::kGated>, 256, 2, p, n, stream, launches);
+    return choose(kGated, p, n).tiling->launch({p, n, stream, launches});
 }
 
 hipError_t launch_block_gate_grad(const BlockProblem *p, uint32_t n, bool, hipStream_t stream, uint64_t *launches)
 {
-    return launch_block<64, 128>(block_stream<64, 128, 2, 2, 3, Epilogue::kGateGrad>, 256, 2, p, n, stream, launches);
+    return choose(kGateGrad, p, n).tiling->launch({p, n, stream, launches});
 }
 
-hipError_t launch_block_plain_t(const BlockProblem *p, uint32_t n, bool, hipStream_t stream, uint64_t *launches)
+hipError_t launch_block_plain_t(const BlockProblem *p, uint32_t n, bool cached, hipStream_t stream, uint64_t *launches)
 {
-    return launch_block<64, 128>(block_stream<64, 128, 2, 2, 3, Epilogue::kPlainT>, 256, 2, p, n, stream, launches);
+    if (n == 0) return hipSuccess;
+    const Choice large = choose(kInputLarge, p, n);
+    if (large.ns < choose(kInputRing, p, n).ns) return large.tiling->launch({p, n, stream, launches});
+    std::vector<Problem> q;
+    q.reserve(n);
+    for (uint32_t i = 0; i < n; ++i) q.push_back({p[i].W, p[i].X, p[i].Y, nullptr, p[i].M, p[i].K, p[i].N, kOutBf16});
+    return launch_grouped_bf16(q.data(), n, true, cached, stream, launches);
 }
 
 // ---- slope of a dense layer -----------------------------------------------------------------------------------------------------
-// dZ = dY * act'(Z), and the column sums of dZ before its rounding: a workgroup takes 16 rows of 1024 columns, a thread four columns of
-// them, one after the other, so that a sum's order is that of the rows.  Bound by memory: 8 bytes an element (2 and 4 read, 2 written).
+// dZ = dY * act'(Z), and the column sums of dZ before its rounding.  A workgroup takes 16 rows of 512 columns, a wavefront four of the rows, a lane
+// eight columns; all of a lane's loads are on their way together.  The four wavefronts' sums are added in the order of the rows.  Bound by memory:
+// 8 bytes an element (2 and 4 read, 2 written).
 struct SlopeArgs {
     uint32_t n, tiles, pad[2];
     uint32_t first[kBlockProblems];
     SlopeProblem p[kBlockProblems];
 };
 static_assert(sizeof(SlopeArgs) <= 4096, "kernel arguments are limited to 4 KB");
-constexpr uint32_t kSlopeCols = 1024;
+constexpr uint32_t kSlopeCols = 512, kSlopeWaveRows = kSlopeRows / kWaves;
 
-__global__ __launch_bounds__(256) void block_slope(SlopeArgs a)
+__global__ __launch_bounds__(64 * kWaves) void block_slope(SlopeArgs a)
 {
+    __shared__ float part[kWaves][8][64];
     SlopeProblem p;
     const uint32_t t = find_owner(a.first, a.p, blockIdx.x, p), ct = (p.N + kSlopeCols - 1) / kSlopeCols;
-    const uint32_t block = t / ct, row0 = block * kSlopeRows, c = (t % ct) * kSlopeCols + 4 * threadIdx.x;
-    if (c >= p.N) return;
-    const uint32_t rows = min(kSlopeRows, p.M - row0);
-    const size_t corner = (size_t)row0 * p.N + c;
-    const Global<uint16_t> *dY = (const Global<uint16_t> *)p.dY + corner;
-    const Global<float> *Z = (const Global<float> *)p.Z + corner;
-    Global<uint16_t> *dZ = (Global<uint16_t> *)p.dZ + corner;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t r = 0; r < rows; ++r) {
-        const u32x2 w = *(const Global<u32x2> *)(dY + (size_t)r * p.N);
-        float v[4] = {bf16_low(w[0]), bf16_high(w[0]), bf16_low(w[1]), bf16_high(w[1])};
-        if (p.Z) {
-            const f32x4 z = *(const Global<f32x4> *)(Z + (size_t)r * p.N);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t block = t / ct, row0 = block * kSlopeRows + wave * kSlopeWaveRows, c = (t % ct) * kSlopeCols + 8 * lane;
+    const bool in = c < p.N;
+    const Global<uint16_t> *dY = (const Global<uint16_t> *)p.dY + (in ? c : 0);
+    const Global<float> *Z = (const Global<float> *)p.Z + (in ? c : 0);
+    u32x4 w[kSlopeWaveRows];
+    f32x4 z[kSlopeWaveRows][2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] *= slope_fine(z[e], p.act);
+    for (uint32_t r = 0; r < kSlopeWaveRows; ++r) {
+        const size_t at = (size_t)min(row0 + r, p.M - 1) * p.N;      // rows past the last: read again, not used
+        w[r] = *(const Global<u32x4> *)(dY + at);
+        if (!p.Z) continue;
+        z[r][0] = *(const Global<f32x4> *)(Z + at);
+        z[r][1] = *(const Global<f32x4> *)(Z + at + 4);
+    }
+    float sum[8] = {};
+#pragma unroll
+    for (uint32_t r = 0; r < kSlopeWaveRows; ++r) {
+        if (row0 + r >= p.M) break;
+        float v[8], slope[8], unused[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[e] = e & 1 ? bf16_high(w[r][e / 2]) : bf16_low(w[r][e / 2]);
+            slope[e] = z[r][e / 4][e & 3];
+        }
+        if (p.Z) {
+            float at[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) at[e] = slope[e];
+            activate_with_slope(at, unused, slope, p.act);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= slope[e];
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += v[e];
-        if (p.dZ) *(Global<u32x2> *)(dZ + (size_t)r * p.N) = u32x2{bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3])};
+        for (int e = 0; e < 8; ++e) sum[e] += v[e];
+        if (p.dZ && in)
+            *(Global<u32x4> *)((Global<uint16_t> *)p.dZ + (size_t)(row0 + r) * p.N + c) =
+                u32x4{bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]), bf16_pack(v[4], v[5]), bf16_pack(v[6], v[7])};
     }
     if (!p.db) return;
-    float *to = p.M <= kSlopeRows ? p.db : p.partial + (size_t)block * p.N;
-    *(Global<f32x4> *)((Global<float> *)to + c) = sum;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[wave][e][lane] = sum[e];
+    __syncthreads();
+    // thread: two of the 512 columns, which lie at [wave][column % 8][column / 8]
+    Global<float> *to = (Global<float> *)(p.M <= kSlopeRows ? p.db : p.partial + (size_t)block * p.N);
+#pragma unroll
+    for (uint32_t i = 0; i < kSlopeCols / 256; ++i) {
+        const uint32_t column = 256 * i + threadIdx.x, n = (t % ct) * kSlopeCols + column;
+        float s = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kWaves; ++q) s += part[q][column & 7][column >> 3];
+        if (n < p.N) to[n] = s;
+    }
 }
 
-// db of jobs of more than 16 rows: the blocks' sums, in row order.
+// db of jobs of more than 16 rows: the blocks' sums.  A workgroup takes 64 columns, 16 threads four of them each, and thread group g the blocks g, g + 16, ..;
+// the groups are added in order.
 __global__ __launch_bounds__(256) void block_column_sums(SlopeArgs a)
 {
+    __shared__ float part[16][64];
     SlopeProblem p;
-    const uint32_t c = find_owner(a.first, a.p, blockIdx.x, p) * 256u + threadIdx.x;
-    if (c >= p.N) return;
+    const uint32_t c0 = find_owner(a.first, a.p, blockIdx.x, p) * 64u, group = threadIdx.x >> 4, c = c0 + 4 * (threadIdx.x & 15);
     const uint32_t blocks = (p.M + kSlopeRows - 1) / kSlopeRows;
-    float sum = 0.0f;
-    for (uint32_t b = 0; b < blocks; ++b) sum += ((const Global<float> *)p.partial)[(size_t)b * p.N + c];
-    ((Global<float> *)p.db)[c] = sum;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (c < p.N) {
+#pragma unroll 4
+        for (uint32_t b = group; b < blocks; b += 16) sum += *(const Global<f32x4> *)((const Global<float> *)p.partial + (size_t)b * p.N + c);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) part[group][4 * (threadIdx.x & 15) + e] = sum[e];
+    __syncthreads();
+    if (threadIdx.x >= 64 || c0 + threadIdx.x >= p.N) return;
+    float s = 0.0f;
+#pragma unroll
+    for (int g = 0; g < 16; ++g) s += part[g][threadIdx.x];
+    ((Global<float> *)p.db)[c0 + threadIdx.x] = s;
 }
 
 hipError_t launch_block_slope(const SlopeProblem *p, uint32_t n, hipStream_t stream, uint64_t *launches)
@@ -124,7 +435,7 @@ hipError_t launch_block_slope(const SlopeProblem *p, uint32_t n, hipStream_t str
             hipLaunchKernelGGL(block_slope, dim3((uint32_t)tiles), dim3(256), 0, stream, a);
             if (launches) *launches += 1;
         }
-        const uint64_t sums = fill_group(a, p + at, count, [](const SlopeProblem &q) { return q.db && q.M > kSlopeRows ? (uint64_t)(q.N + 255) / 256 : 0; });
+        const uint64_t sums = fill_group(a, p + at, count, [](const SlopeProblem &q) { return q.db && q.M > kSlopeRows ? (uint64_t)(q.N + 63) / 64 : 0; });
         if (sums) {
             hipLaunchKernelGGL(block_column_sums, dim3((uint32_t)sums), dim3(256), 0, stream, a);
             if (launches) *launches += 1;

@@ -63,10 +63,26 @@ __device__ inline double sum_of_squares(const void *g, uint64_t begin, uint64_t 
 {
     constexpr uint32_t kVec = BF16 ? 8 : 4, kLoads = 4;
     double s[4] = {0, 0, 0, 0};
+    // Squares of bf16 numbers are exact in float, and eight of them are added there if that can neither overflow nor lose all of them: 64-bit conversions
+    // of every element take longer than reading it.
     auto add = [&](u32x4 w) {
         if constexpr (BF16) {
+            float v[8], most = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] += square(bf16_low(w[i])) + square(bf16_high(w[i]));
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = bf16_low(w[i]);
+                v[2 * i + 1] = bf16_high(w[i]);
+                most = fmaxf(most, fmaxf(fabsf(v[2 * i]), fabsf(v[2 * i + 1])));
+            }
+            float q = v[0] * v[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) q = fmaf(v[i], v[i], q);
+            if (most > 0x1p-50f && most < 0x1p50f) {      // not so of a NaN beside ordinary numbers: q is one then
+                s[0] += (double)q;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] += square(v[2 * i]) + square(v[2 * i + 1]);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[i] += square(as_float(w[i]));
@@ -136,17 +152,25 @@ __device__ inline void apply_clip(const ClipEntry &t, uint64_t begin, uint64_t e
         } else if constexpr (BF16) ((Global<uint16_t> *)t.g)[i] = (uint16_t)bf16_bits(v);
         else ((Global<float> *)t.g)[i] = v;
     };
+    constexpr uint32_t kLoads = SGD ? 2 : 4;      // vectors on their way per thread
     const uint64_t whole = begin + (end - begin) / kVec * kVec;
-    for (uint64_t i = begin + (uint64_t)kVec * threadIdx.x; i < whole; i += kVec * 256) {
-        const u32x4 w = *(const Global<u32x4> *)((const Global<char> *)t.g + i * (BF16 ? 2 : 4));
+    struct Vec { u32x4 g; f32x4 m[SGD ? kVec / 4 : 1]; };
+    auto load = [&](Vec &x, uint64_t i) {
+        x.g = *(const Global<u32x4> *)((const Global<char> *)t.g + i * (BF16 ? 2 : 4));
+        if constexpr (SGD) {
+#pragma unroll
+            for (uint32_t q = 0; q < kVec / 4; ++q) x.m[q] = *(const Global<f32x4> *)((const Global<float> *)t.wm + i + 4 * q);
+        }
+    };
+    auto store = [&](const Vec &x, uint64_t i) {
         float v[kVec];
 #pragma unroll
-        for (uint32_t e = 0; e < kVec; ++e) v[e] = __fmul_rn(BF16 ? (e & 1 ? bf16_high(w[e / 2]) : bf16_low(w[e / 2])) : as_float(w[e & 3]), c);
+        for (uint32_t e = 0; e < kVec; ++e) v[e] = __fmul_rn(BF16 ? (e & 1 ? bf16_high(x.g[e / 2]) : bf16_low(x.g[e / 2])) : as_float(x.g[e & 3]), c);
         if constexpr (SGD) {
             uint32_t b[kVec / 2];
 #pragma unroll
             for (uint32_t q = 0; q < kVec; q += 4) {
-                f32x4 m = *(const Global<f32x4> *)((const Global<float> *)t.wm + i + q);
+                f32x4 m = x.m[q / 4];
 #pragma unroll
                 for (uint32_t e = 0; e < 4; ++e) m[e] = __fsub_rn(m[e], __fmul_rn(lr, v[q + e]));      // one rounding each
                 *(Global<f32x4> *)((Global<float> *)t.wm + i + q) = m;
@@ -160,6 +184,21 @@ __device__ inline void apply_clip(const ClipEntry &t, uint64_t begin, uint64_t e
         } else {
             *(Global<f32x4> *)((Global<float> *)t.g + i) = f32x4{v[0], v[1], v[2], v[3]};
         }
+    };
+    constexpr uint64_t kStride = kVec * 256;
+    uint64_t i = begin + (uint64_t)kVec * threadIdx.x;
+    for (; i + (kLoads - 1) * kStride < whole; i += kLoads * kStride) {
+        Vec x[kLoads];
+#pragma unroll
+        for (uint32_t l = 0; l < kLoads; ++l) load(x[l], i + l * kStride);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t l = 0; l < kLoads; ++l) store(x[l], i + l * kStride);
+    }
+    for (; i < whole; i += kStride) {
+        Vec x;
+        load(x, i);
+        store(x, i);
     }
     if (whole + threadIdx.x < end) one(whole + threadIdx.x);
 }

@@ -51,17 +51,19 @@ struct NarrowTile {
         (one(std::integral_constant<uint32_t, sizeof...(I) - 1 - I>{}), ...);
     }
 
-    __device__ static void run(const Problem &p, const Tile tile, unsigned char *smem)
+    // The product alone: own[t * NB + j] is the sum of row m0 + 16 t + 4 (lane / 16) + wave, column n0 + 16 j + lane % 16.  `second` (PAIRS): the tile is
+    // 8 * NB columns of N and the same ones `second` bytes further on, which are the upper half of j; pitch: bytes between k-rows.
+    template <bool PAIRS, bool ZEROS>
+    __device__ static void sums(const void *W, const void *X, uint32_t M, uint32_t K, uint32_t N, bool blocked_in, bool strip, uint32_t pitch, uint32_t second,
+                                const Tile tile, unsigned char *smem, float (&own)[kNacc])
     {
-        const uint32_t M = p.M, K = p.K, N = p.N;
+        static_assert(!PAIRS || NB % 2 == 0, "as many columns of each half");
         const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const bool blocked_in = (p.flags & kInBlocked) != 0, strip = (p.flags & kStripW) != 0;
         const uint32_t xtiles = (M + 15) / 16;
 
         // Requests of a k-step: NB kilobytes of weights, 32 / NB rows each, then a kilobyte of activations per row tile.
         constexpr uint32_t kLanes = 2 * NB;      // lanes of a k-row
-        const uint32_t pitch = strip ? 256u : N * 2u;
         const uint32_t first_col = strip ? (tile.n0 & 127u) : tile.n0;
         uint32_t w_off[NB], krow[NB];
 #pragma unroll
@@ -69,16 +71,20 @@ struct NarrowTile {
             const uint32_t at = 64u * i + lane;
             krow[i] = row_at(at / kLanes);
             const uint32_t col = 8u * ((at % kLanes) ^ chunk_swizzle(krow[i]));
-            w_off[i] = tile.n0 + col < N ? krow[i] * pitch + (first_col + col) * 2u + (strip && first_col + col >= 128u ? (K - 1) * 256u : 0u) : kOutside;
+            if constexpr (PAIRS) {
+                const uint32_t half = col >= 8u * NB ? 1u : 0u, mine = tile.n0 + col - half * 8u * NB;
+                w_off[i] = mine < N ? krow[i] * pitch + mine * 2u + half * second : kOutside;
+            } else w_off[i] = tile.n0 + col < N ? krow[i] * pitch + (first_col + col) * 2u + (strip && first_col + col >= 128u ? (K - 1) * 256u : 0u) : kOutside;
         }
-        uint64_t w_base = (uint64_t)(uintptr_t)p.W + (strip ? (uint64_t)(tile.n0 & ~127u) * K * 2u : 0);
-        uint64_t x_base = (uint64_t)(uintptr_t)p.X;
+        uint64_t w_base = (uint64_t)(uintptr_t)W + (strip ? (uint64_t)(tile.n0 & ~127u) * K * 2u : 0);
+        uint64_t x_base = (uint64_t)(uintptr_t)X;
         uint32_t x_off[MT];
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             // a row tile that the job does not have (its rows are never stored) reads the last one instead
             const uint32_t row = tile.m0 + 16u * t + c, tt = min((uint32_t)t, xtiles - 1);
-            x_off[t] = blocked_in ? tt * 1024u + 16u * lane : (row < M ? row : M - 1) * K * 2u + 16u * g;
+            if (ZEROS) x_off[t] = row < M ? row * K * 2u + 16u * g : kOutside;
+            else x_off[t] = blocked_in ? tt * 1024u + 16u * lane : (row < M ? row : M - 1) * K * 2u + 16u * g;
         }
         const uint64_t w_step = (uint64_t)32u * pitch, x_step = blocked_in ? xtiles * 1024u : 64u;
         const uint32_t nsteps = (K + 31) / 32;
@@ -159,9 +165,18 @@ struct NarrowTile {
         // the last ones, all requested: nothing is left in flight after them
         drain(std::make_index_sequence<D / STEP>{}, groups, multiply);
 
-        float own[kNacc];
         if (kAlias) __syncthreads();
         reduce_scatter<kNacc>(acc, own, (float *)(smem + kSumsAt));
+    }
+
+    __device__ static void run(const Problem &p, const Tile tile, unsigned char *smem)
+    {
+        const uint32_t M = p.M, N = p.N, xtiles = (M + 15) / 16;
+        const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const bool strip = (p.flags & kStripW) != 0;
+        float own[kNacc];
+        sums<false, false>(p.W, p.X, M, p.K, N, (p.flags & kInBlocked) != 0, strip, strip ? 256u : N * 2u, 0, tile, smem, own);
         const uint32_t act = p.flags & 0xffu;
 #pragma unroll
         for (int t = 0; t < MT; ++t)

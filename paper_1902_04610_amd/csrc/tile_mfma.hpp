@@ -550,12 +550,12 @@ struct TilePair {
 // tiles keeps it full through the epilogues.  One barrier per slab: after it slab s has landed for everyone
 // and everyone has left the stage of slab s - 1, which is requested into at once.  HALVES: two sums per output, over the first and
 // over the second two k-steps of every slab, added at the end of a tile.
-template <int BM, int BN, int WM, int WN, bool TRN, int D, bool HALVES = false, bool PAIRS = false>
+template <int BM, int BN, int WM, int WN, bool TRN, int D, bool HALVES = false, bool PAIRS = false, bool ONCE = false>
 struct TileStream {
     static constexpr int kWavesT = WM * WN, kThreads = 64 * kWavesT;
     static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;
     using SM = OperandStream<BM, false, kWavesT, D>;
-    using SN = OperandStream<BN, TRN, kWavesT, D, kSlab, false, PAIRS>;
+    using SN = OperandStream<BN, TRN, kWavesT, D, kSlab, ONCE, PAIRS>;
     static constexpr uint32_t kLds = SM::kRing + SN::kRing;
     static constexpr int kBehind = (D - 2) * (SM::I + SN::I);
     static_assert(kLds <= 160 * 1024 && kBehind <= 63, "LDS of a compute unit, largest count of s_waitcnt");
@@ -660,6 +660,145 @@ struct TileStream {
                 break;
             }
             cur = walk.place(cur_id);          // the requests may be more than one tile ahead
+        }
+    }
+};
+
+// Both operands major (X . W^T, the weights' rows along the contraction): the M side has three slabs, the N side two.  One barrier
+// per slab, before k-step 3: by then slab t has been read, and k-step 3 requests slab t + 2 into the N side's stage of it; the M side's
+// stage has been free for a slab, and its slab t + 2 is requested in k-steps 1 and 2.  So the N side's requests, the younger ones, have three k-steps
+// until they are waited for, and what may be in flight then is the M side's four k-steps' worth alone.
+template <int BM, int BN, int WM, int WN>
+struct TileRows {
+    static constexpr int kWavesT = WM * WN, kThreads = 64 * kWavesT;
+    static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;
+    using SM = OperandStream<BM, false, kWavesT, 3>;
+    using SN = OperandStream<BN, false, kWavesT, 2>;
+    static constexpr uint32_t kLds = SM::kRing + SN::kRing;
+    static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+    static_assert(FM * FN > 1, "a k-step places its reads between its multiplies");
+    typedef f32x16 Acc[FN][FM];
+
+    template <typename Walk>
+    __device__ static void run(const Walk &walk, unsigned char *smem)
+    {
+        const int lane = threadIdx.x & 63;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint32_t wm = wave / WN, wn = wave % WN;
+        const uint32_t lds_m = lds_address(smem), lds_n = lds_m + SM::kRing;
+        Fragments<BM, false, FM> fm;
+        Fragments<BN, false, FN> fn;
+        fm.init(wm * (32u * FM), lane);
+        fn.init(wn * (32u * FN), lane);
+
+        const uint32_t tiles = walk.tiles();
+        uint32_t id = blockIdx.x;                // of the tile that the M stream walks towards
+        typename Walk::Place ahead = walk.place(id), cur = ahead;
+        uint32_t cur_id = id;
+        SM sm;
+        SN sn;
+        sm.start(lane);
+        sn.start(lane);
+        sm.locate(walk.m(ahead), ahead.m0, wave);
+        sn.locate(walk.n(ahead), ahead.n0, wave);
+        // crossed into right behind the last request of a tile, the M side first
+        auto advance_m = [&]() {
+            sm.advance();
+            if (sm.slabs_left != 0) return;
+            id += gridDim.x;
+            if (id < tiles) {
+                ahead = walk.place(id);
+                sm.locate(walk.m(ahead), ahead.m0, wave);
+            } else sm.stop();
+        };
+        auto advance_n = [&]() {
+            sn.advance();
+            if (sn.slabs_left != 0) return;
+            if (id < tiles) sn.locate(walk.n(ahead), ahead.n0, wave);
+            else sn.stop();
+        };
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int i = 0; i < SM::I; ++i) sm.fetch(i, lds_m, wave);
+            advance_m();
+#pragma unroll
+            for (int i = 0; i < SN::I; ++i) sn.fetch(i, lds_n, wave);
+            advance_n();
+        }
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(SM::I + SN::I) : "memory");
+
+        Acc acc;
+        bf16x8 a[2][FN], b[2][FM];
+        uint32_t at_m = 0, at_n = 0;             // ring offsets of the slab that is read
+        auto read = [&](int r, int ks, int set) {
+            const unsigned char *base_m = smem + at_m, *base_n = smem + SM::kRing + at_n;
+            if (r == 0) b[set][0] = fm.read(base_m, ks, 0);
+            else if (r == 1) a[set][0] = fn.read(base_n, ks, 0);
+            else if (r < FM + 1) b[set][r - 1] = fm.read(base_m, ks, r - 1);
+            else if (r < FM + FN) a[set][r - FM] = fn.read(base_n, ks, r - FM);
+        };
+        // k-step q: its multiplies, with the reads of the next one and the requests of q between them
+        auto step = [&](int q) {
+            const int set = q & 1;
+            const int begin = q == 2 ? SM::I / 2 : 0, end = q == 1 ? SM::I / 2 : q == 2 ? SM::I : q == 3 ? SN::I : 0;
+            int r = 0, f = begin;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[set][j], b[set][i], acc[j][i], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    const int n = j * FM + i + 1;
+                    const int until = (n * (FM + FN) + FM * FN - 2) / (FM * FN - 1);
+#pragma unroll
+                    for (; r < until && r < FM + FN; ++r) read(r, (q + 1) & 3, set ^ 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                    const int upto = begin + (n * (end - begin) + FM * FN - 1) / (FM * FN);
+#pragma unroll
+                    for (; f < upto; ++f) {
+                        if (q == 3) sn.fetch(f, lds_n, wave);
+                        else sm.fetch(f, lds_m, wave);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        };
+        bool landed = false;                     // everything requested up to the last epilogue
+
+#pragma unroll
+        for (int r = 0; r < FM + FN; ++r) read(r, 0, 0);
+        for (;;) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[j][i][r] = 0.f;
+            uint32_t left = __builtin_amdgcn_readfirstlane(max((cur.depth + kSlab - 1) / kSlab, kMinSlabs));
+#pragma clang loop unroll(disable)
+            do {
+                step(0);
+                step(1);
+                step(2);
+                advance_m();
+                if (landed) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SM::I) : "memory");
+                landed = false;
+                at_m = at_m + SM::kBytes == (uint32_t)SM::kRing ? 0u : at_m + SM::kBytes;
+                at_n = at_n + SN::kBytes == (uint32_t)SN::kRing ? 0u : at_n + SN::kBytes;
+                step(3);
+                advance_n();
+            } while (--left != 0);
+            walk.finish(cur, acc, typename Walk::Held{}, wm * (32u * FM), wn * (32u * FN), fresh_lane(), [&]() {
+                if (!landed) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                landed = true;
+            });
+            cur_id += gridDim.x;
+            if (cur_id >= tiles) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may arrive in LDS after this workgroup
+                break;
+            }
+            cur = ahead;         // the M side has crossed into it and no further
         }
     }
 };
