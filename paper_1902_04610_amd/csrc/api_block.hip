@@ -317,7 +317,7 @@ int32_t salus_grouped_dense_backward(salus_pool_t *pool, const salus_dense_grad_
 uint64_t salus_clip_work_bytes(const salus_clip_tensor *tensors, uint32_t n_tensors)
 {
     if (!tensors) return 0;
-    return 8 * clip_work_doubles(n_tensors, [&](uint32_t i) { return tensors[i].count; });
+    return 8 * clip_sums(n_tensors, [&](uint32_t i) { return tensors[i].count; });
 }
 
 int32_t salus_grouped_clip(salus_pool_t *pool, const salus_clip_desc *descs, uint32_t n, void *stream)

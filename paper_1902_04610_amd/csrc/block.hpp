@@ -465,26 +465,21 @@ struct ClipJob {
     uint32_t n_tensors;
     float max_norm, lr;
     float *norm;
-    double *work;        // clip_work_doubles()
+    double *work;        // clip_sums()
 };
-// A tensor is read in chunks of kClipChunk << shift elements, each of which has one sum in the job's work area: the smallest chunks that leave
-// a job at most kClipSums of them beside one per tensor.  count(i): elements of tensor i.  Returns the shift.
-constexpr uint32_t kClipChunkBits = 12, kClipSums = 1024;
-inline uint64_t clip_chunks(uint64_t count, uint32_t shift) { return (count + (1ull << (kClipChunkBits + shift)) - 1) >> (kClipChunkBits + shift); }
+// A tensor is read in chunks of 4096 elements.  A job's tensors go in groups of kClipTensors, and a group has a sum of squares for each of its workgroups: one per
+// chunk, but no more than kClipSums.  clip_sums: those of a job, whose tensor i has count(i) elements.
+constexpr uint32_t kClipChunkBits = 12, kClipSums = 1024, kClipTensors = 64;
+inline uint64_t clip_chunks(uint64_t count) { return (count + (1ull << kClipChunkBits) - 1) >> kClipChunkBits; }
 template <typename Count>
-inline uint32_t clip_shift(uint32_t n, Count count, uint64_t *sums)
+inline uint64_t clip_sums(uint32_t n, Count count)
 {
-    for (uint32_t shift = 0;; ++shift) {
-        *sums = 0;
-        for (uint32_t i = 0; i < n; ++i) *sums += clip_chunks(count(i), shift);
-        if (*sums <= (uint64_t)kClipSums + n || shift == 48) return shift;
+    uint64_t sums = 0;
+    for (uint32_t i = 0; i < n; i += kClipTensors) {
+        uint64_t chunks = 0;
+        for (uint32_t k = i; k < n && k < i + kClipTensors; ++k) chunks += clip_chunks(count(k));
+        sums += chunks < kClipSums ? chunks : kClipSums;
     }
-}
-template <typename Count>
-inline uint64_t clip_work_doubles(uint32_t n, Count count)
-{
-    uint64_t sums;
-    clip_shift(n, count, &sums);
     return sums;
 }
 hipError_t launch_clip(const ClipJob *jobs, uint32_t n, bool sgd, hipStream_t stream, uint64_t *launches);
