@@ -9,7 +9,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsalus.so")
 SOURCES = ["api.hip", "api_block.hip", "kernels_copy.hip", "kernels_gemm.hip", "kernels_chain.hip", "kernels_gemm_tiled.hip", "kernels_train.hip",
-           "kernels_block.hip", "kernels_weight_grad.hip", "kernels_clip.hip", "pool_core.cpp"]
+           "kernels_block.hip", "kernels_gradients.hip", "kernels_clip.hip", "pool_core.cpp"]
 
 
 def build(verbose=False, extra_flags=(), out=LIB):

@@ -162,8 +162,8 @@ int32_t gated_backward(salus_pool_t *pool, const salus_gated_grad_desc *descs, u
     const bool cached = weights_cached(pool);
     uint64_t *count = launch_counter(pool);
     hipError_t e = launch_block_gate_grad(gate.data(), n, cached, stream, count);
-    if (e == hipSuccess) e = launch_block_plain_t(input.data(), (uint32_t)input.size(), cached, stream, count);
-    if (e == hipSuccess) e = launch_weight_grad(weight.data(), (uint32_t)weight.size(), stream, count);
+    if (e == hipSuccess)
+        e = launch_gradients(input.data(), (uint32_t)input.size(), weight.data(), (uint32_t)weight.size(), nullptr, 0, cached, stream, count);
     return launched(pool, e);
 }
 
@@ -230,8 +230,9 @@ int32_t dense_backward(salus_pool_t *pool, const salus_dense_grad_desc *descs, u
     if (rc) return rc;
     uint64_t *count = launch_counter(pool);
     hipError_t e = launch_block_slope(slope.data(), n, stream, count);
-    if (e == hipSuccess) e = launch_block_plain_t(input.data(), (uint32_t)input.size(), weights_cached(pool), stream, count);
-    if (e == hipSuccess) e = launch_weight_grad(weight.data(), n, stream, count);
+    slope.erase(std::remove_if(slope.begin(), slope.end(), [](const SlopeProblem &q) { return !q.db || q.M <= kSlopeRows; }), slope.end());
+    if (e == hipSuccess)
+        e = launch_gradients(input.data(), (uint32_t)input.size(), weight.data(), n, slope.data(), (uint32_t)slope.size(), weights_cached(pool), stream, count);
     return launched(pool, e);
 }
 

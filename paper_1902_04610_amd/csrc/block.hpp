@@ -344,21 +344,22 @@ __device__ inline void finish_gate_grad(const BlockProblem &p, const Part &at, u
 // ---- tile walks (tile_mfma.hpp) ---------------------------------------------------------------------------------------------------
 // Gated: a tile of BN columns is BN / 2 of the gate's and the same BN / 2 of the other half's, sixteen and sixteen by turns
 // (OperandStream's PAIRS), so that a lane has a gate's sum and its partner's in registers r and r + 8 of one block.
-template <int BM, int BN, Epilogue E>
+template <int BM, int BN, Epilogue E, typename Args = BlockArgs>
 struct BlockWalk {
+    static constexpr uint32_t kProblems = sizeof(Args::first) / 4;
     static constexpr uint32_t kCols = E == Epilogue::kGated ? BN / 2 : BN;      // of the output
     static constexpr bool kTransposed = E == Epilogue::kGateGrad || E == Epilogue::kPlainT;
-    const BlockArgs &a;
+    const Args &a;
     const uint32_t first;      // lane i: the first tile of problem i
     struct Place { int problem; uint32_t m0, n0, depth; };
-    __device__ explicit BlockWalk(const BlockArgs &args) : a(args), first(args.first[min(threadIdx.x & 63, kBlockProblems - 1)]) {}
+    __device__ explicit BlockWalk(const Args &args) : a(args), first(args.first[min(threadIdx.x & 63, kProblems - 1)]) {}
     __device__ uint32_t tiles() const { return a.tiles; }
     // Tiles of one job in bands of 8 row tiles, column tiles inside a band: the tiles an XCD runs at a time then share 8
     // slabs of X and 4 - 8 slabs of W in its L2.
     __device__ Place place(uint32_t tile_id) const
     {
         const uint32_t id = xcd_remap(tile_id, a.tiles);
-        const int g = __builtin_amdgcn_readfirstlane(wave_find_range(first, id, (threadIdx.x & 63) < kBlockProblems));
+        const int g = __builtin_amdgcn_readfirstlane(wave_find_range(first, id, (threadIdx.x & 63) < kProblems));
         const BlockProblem &p = a.p[g];
         const uint32_t t = id - __builtin_amdgcn_readlane(first, g), rt = (p.M + BM - 1) / BM, ct = (p.N + kCols - 1) / kCols;
         const uint32_t band = t / (8u * ct), local = t - band * 8u * ct, rows = min(8u, rt - band * 8u);
@@ -429,9 +430,8 @@ struct BlockWalk {
 hipError_t launch_block_dense(const BlockProblem *p, uint32_t n, bool cached, hipStream_t stream, uint64_t *launches);
 hipError_t launch_block_gated(const BlockProblem *p, uint32_t n, bool cached, hipStream_t stream, uint64_t *launches);
 hipError_t launch_block_gate_grad(const BlockProblem *p, uint32_t n, bool cached, hipStream_t stream, uint64_t *launches);
-hipError_t launch_block_plain_t(const BlockProblem *p, uint32_t n, bool cached, hipStream_t stream, uint64_t *launches);
 
-// dZ = dY * act'(Z) of a dense layer, and the column sums of it.
+// dZ = dY * act'(Z) of a dense layer, and the column sums of it: db itself for up to kSlopeRows rows, else those of blocks of as many.
 struct SlopeProblem {
     const void *dY;      // M x N bf16
     const float *Z;      // M x N, or null (no activation)
@@ -450,7 +450,10 @@ struct WeightGradProblem {
     void *dW;            // K x N bf16
     uint32_t M, K, N;
 };
-hipError_t launch_weight_grad(const WeightGradProblem *p, uint32_t n, hipStream_t stream, uint64_t *launches);
+// What a backward pass ends with, none of which waits for another: input gradients (BlockProblem as for a transposed product), weight gradients and the
+// column sums that launch_block_slope left (db of jobs of more than kSlopeRows rows).  Any of the counts may be zero.
+hipError_t launch_gradients(const BlockProblem *input, uint32_t n_input, const WeightGradProblem *weight, uint32_t n_weight, const SlopeProblem *sums, uint32_t n_sums,
+                            bool cached, hipStream_t stream, uint64_t *launches);
 
 // ---- gradient clipping ------------------------------------------------------------------------------------------------------------
 struct ClipTensor {

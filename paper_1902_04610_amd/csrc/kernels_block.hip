@@ -3,38 +3,11 @@
 // the product of the halves, the residual, the gate's derivative) happens on its float sums on the way to memory (block.hpp), so that
 // a round of dense layers is one launch and one of gated blocks is two.
 #include <algorithm>
-#include <type_traits>
-#include <vector>
 
-#include "block.hpp"
+#include "block_launch.hpp"
 #include "narrow_tile.hpp"
 
 namespace salus {
-
-// 64-row tiles, operands through an LDS ring (TileStream), two workgroups per compute unit.  Right for every size: rows and columns outside
-// are neither fetched nor stored.
-template <int BM, int BN, int WM, int WN, int D, Epilogue E, bool ONCE = false>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN / 2) void block_stream(BlockArgs a)
-{
-    using Walk = BlockWalk<BM, BN, E>;
-    using T = TileStream<BM, BN, WM, WN, !Walk::kTransposed, D, false, E == Epilogue::kGated, ONCE>;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[T::kLds];
-    const Walk walk(a);
-    T::run(walk, smem);
-}
-
-// Large tiles (TileMfma, TilePair, TileRows): where a weight is used by 128 rows and more, or comes in whole rounds of tiles.
-template <int BM, int BN, int WM, int WN, Epilogue E, bool ONCE = false>
-__global__ __launch_bounds__(64 * WM * WN, 2) void block_tiled(BlockArgs a)
-{
-    using Walk = BlockWalk<BM, BN, E>;
-    constexpr bool kPairs = E == Epilogue::kGated;
-    using T = std::conditional_t<Walk::kTransposed, TileRows<BM, BN, WM, WN>,
-                                 std::conditional_t<BM * BN == 128 * 256, TilePair<BM, BN, WM, WN, ONCE, kPairs>, TileMfma<BM, BN, WM, WN, false, true, kPairs>>>;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[T::kLds];
-    const Walk walk(a);
-    T::run(walk, smem);
-}
 
 // Few rows (at most 16 MT): tiles of 16 NB columns of weights, K split over the four wavefronts of a workgroup, weights straight into an LDS ring per
 // wavefront (NarrowTile).  Gated: half the columns are the gate's.  TWO: two workgroups per compute unit.
@@ -163,71 +136,6 @@ __global__ __launch_bounds__(kGemmThreads) void block_gate_grad_narrow(Args a)
     else narrow_gate_grad<MT, CPL, 2>(p, tile, lds);
 }
 
-// Launches of at most as many problems as Args holds: bm rows and `cols` output columns a tile, at most `grid` workgroups (0: one per tile).
-template <typename Args>
-static hipError_t launch_block(void (*kernel)(Args), int threads, uint32_t bm, uint32_t cols, uint32_t grid, const BlockProblem *p, uint32_t n,
-                               hipStream_t stream, uint64_t *launches)
-{
-    constexpr uint32_t kMost = sizeof(Args::first) / 4;
-    for (uint32_t at = 0; at < n; at += kMost) {
-        Args a{};
-        const uint64_t tiles = fill_group(a, p + at, std::min(kMost, n - at),
-                                          [&](const BlockProblem &q) { return (uint64_t)((q.M + bm - 1) / bm) * ((q.N + cols - 1) / cols); });
-        if (tiles == 0) continue;
-        if (tiles > 0x7fffffffull) return hipErrorInvalidValue;
-        hipLaunchKernelGGL(kernel, dim3(grid ? (uint32_t)std::min<uint64_t>(tiles, grid) : (uint32_t)tiles), dim3(threads), 0, stream, a);
-        if (launches) *launches += 1;
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
-}
-
-struct Round {
-    const BlockProblem *p;
-    uint32_t n;
-    hipStream_t stream;
-    uint64_t *launches;
-};
-
-// One way to run a round: tiles of bm rows and `cols` columns of the output, per_cu of them at a time on a compute unit, for rounds whose largest job has
-// more than `above` and at most `upto` rows; how long a launch takes in nanoseconds: fixed + rounds of tiles x (slabs of 64 of the depth x slab + rest).
-struct Tiling {
-    uint32_t bm, cols, per_cu, above, upto, fixed, slab, rest;
-    hipError_t (*launch)(const Round &);
-};
-constexpr uint32_t kAnyRows = ~0u;
-
-static uint64_t launch_ns(const Tiling &t, const BlockProblem *p, uint32_t n)
-{
-    uint64_t tiles = 0, work = 0;
-    for (uint32_t i = 0; i < n; ++i) {
-        const uint64_t count = (uint64_t)((p[i].M + t.bm - 1) / t.bm) * ((p[i].N + t.cols - 1) / t.cols);
-        tiles += count;
-        work += count * ((uint64_t)std::max((p[i].K + kSlab - 1) / kSlab, kMinSlabs) * t.slab + t.rest);
-    }
-    if (tiles == 0) return 0;
-    // a last round that leaves half of the compute units one tile instead of two takes 0.6 of the time of a full one
-    const uint64_t cus = resident_grid(), grid = cus * t.per_cu, last = tiles % grid;
-    const uint64_t tenths = tiles / grid * 10 + (last == 0 ? 0 : t.per_cu == 1 || last > cus ? 10 : 6);
-    return t.fixed + tenths * (work / tiles) / 10;
-}
-
-struct Choice { const Tiling *tiling; uint64_t ns; };
-template <size_t N>
-static Choice choose(const Tiling (&tilings)[N], const BlockProblem *p, uint32_t n)
-{
-    uint32_t rows = 0;
-    for (uint32_t i = 0; i < n; ++i) rows = std::max(rows, p[i].M);
-    Choice best{nullptr, ~0ull};
-    for (const Tiling &t : tilings) {
-        if (rows <= t.above || rows > t.upto) continue;
-        const uint64_t ns = launch_ns(t, p, n);
-        if (ns < best.ns) best = {&t, ns};
-    }
-    return best;
-}
-
 template <int MT, int NB, bool TWO, Epilogue E>
 static hipError_t narrow(const Round &r)
 {
@@ -242,17 +150,6 @@ static hipError_t narrow_grad(const Round &r)
     if (r.n <= kBlockFew) return launch_block<BlockFewArgs>(block_gate_grad_narrow<MT, CPL, BlockFewArgs>, kGemmThreads, 16 * MT, 16 * CPL, 0, r.p, r.n, r.stream, r.launches);
     return launch_block<BlockArgs>(block_gate_grad_narrow<MT, CPL, BlockArgs>, kGemmThreads, 16 * MT, 16 * CPL, 0, r.p, r.n, r.stream, r.launches);
 }
-template <int BM, int BN, int WM, int WN, int D, Epilogue E>
-static hipError_t ring(const Round &r)
-{
-    return launch_block<BlockArgs>(block_stream<BM, BN, WM, WN, D, E>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, 2 * resident_grid(), r.p, r.n, r.stream, r.launches);
-}
-template <int BM, int BN, int WM, int WN, int PER_CU, Epilogue E>
-static hipError_t tiled(const Round &r)
-{
-    return launch_block<BlockArgs>(block_tiled<BM, BN, WM, WN, E>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, PER_CU * resident_grid(), r.p, r.n, r.stream, r.launches);
-}
-
 // Fitted to launches of drawn sizes (1 - 48 jobs of 1 - 4096 rows, widths of 64 - 8192; 210 dense, 105 gated, 61 gate gradients, 100 input gradients, kernel
 // traces of every kind of tile on each of them): off by 6 - 10 % in the median.  The choice is 1.9 % (dense), 2.7 % (gated) and 1.9 % (gate gradients) off the quickest kind on
 // average and 28, 33 and 34 % at most; the best single kind is 38 (64 x 64), 32 (64 x 128) and 25 % (32 x 32) off.  What each is for: narrow tiles fill the chip with few rows, the
@@ -290,17 +187,6 @@ constexpr Tiling kGateGrad[] = {
     {128, 128, 2, 0, kAnyRows, 0, 904, 14890, tiled<128, 128, 2, 2, 2, Epilogue::kGateGrad>},
     {256, 256, 1, 0, kAnyRows, 0, 1074, 19050, tiled<256, 256, 2, 4, 1, Epilogue::kGateGrad>},
 };
-// Input gradients: large tiles, if they are quicker than what the grouped dense layers have for transposed weights (launch_grouped_bf16), for which the ring's
-// tiles stand here.
-constexpr Tiling kInputLarge[] = {
-    {128, 128, 2, 0, kAnyRows, 1400, 886, 3750, tiled<128, 128, 2, 2, 2, Epilogue::kPlainT>},
-    {256, 256, 1, 0, kAnyRows, 0, 1033, 6770, tiled<256, 256, 2, 4, 1, Epilogue::kPlainT>},
-};
-constexpr Tiling kInputRing[] = {
-    {64, 64, 2, 0, kAnyRows, 2100, 405, 1920, nullptr},
-    {64, 128, 2, 0, kAnyRows, 1400, 605, 2940, nullptr},
-};
-
 hipError_t launch_block_dense(const BlockProblem *p, uint32_t n, bool, hipStream_t stream, uint64_t *launches)
 {
     return choose(kDense, p, n).tiling->launch({p, n, stream, launches});
@@ -314,17 +200,6 @@ hipError_t launch_block_gated(const BlockProblem *p, uint32_t n, bool, hipStream
 hipError_t launch_block_gate_grad(const BlockProblem *p, uint32_t n, bool, hipStream_t stream, uint64_t *launches)
 {
     return choose(kGateGrad, p, n).tiling->launch({p, n, stream, launches});
-}
-
-hipError_t launch_block_plain_t(const BlockProblem *p, uint32_t n, bool cached, hipStream_t stream, uint64_t *launches)
-{
-    if (n == 0) return hipSuccess;
-    const Choice large = choose(kInputLarge, p, n);
-    if (large.ns < choose(kInputRing, p, n).ns) return large.tiling->launch({p, n, stream, launches});
-    std::vector<Problem> q;
-    q.reserve(n);
-    for (uint32_t i = 0; i < n; ++i) q.push_back({p[i].W, p[i].X, p[i].Y, nullptr, p[i].M, p[i].K, p[i].N, kOutBf16});
-    return launch_grouped_bf16(q.data(), n, true, cached, stream, launches);
 }
 
 // ---- slope of a dense layer -----------------------------------------------------------------------------------------------------
@@ -399,29 +274,6 @@ __global__ __launch_bounds__(64 * kWaves) void block_slope(SlopeArgs a)
     }
 }
 
-// db of jobs of more than 16 rows: the blocks' sums.  A workgroup takes 64 columns, 16 threads four of them each, and thread group g the blocks g, g + 16, ..;
-// the groups are added in order.
-__global__ __launch_bounds__(256) void block_column_sums(SlopeArgs a)
-{
-    __shared__ float part[16][64];
-    SlopeProblem p;
-    const uint32_t c0 = find_owner(a.first, a.p, blockIdx.x, p) * 64u, group = threadIdx.x >> 4, c = c0 + 4 * (threadIdx.x & 15);
-    const uint32_t blocks = (p.M + kSlopeRows - 1) / kSlopeRows;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    if (c < p.N) {
-#pragma unroll 4
-        for (uint32_t b = group; b < blocks; b += 16) sum += *(const Global<f32x4> *)((const Global<float> *)p.partial + (size_t)b * p.N + c);
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) part[group][4 * (threadIdx.x & 15) + e] = sum[e];
-    __syncthreads();
-    if (threadIdx.x >= 64 || c0 + threadIdx.x >= p.N) return;
-    float s = 0.0f;
-#pragma unroll
-    for (int g = 0; g < 16; ++g) s += part[g][threadIdx.x];
-    ((Global<float> *)p.db)[c0 + threadIdx.x] = s;
-}
-
 hipError_t launch_block_slope(const SlopeProblem *p, uint32_t n, hipStream_t stream, uint64_t *launches)
 {
     for (uint32_t at = 0; at < n; at += kBlockProblems) {
@@ -433,11 +285,6 @@ hipError_t launch_block_slope(const SlopeProblem *p, uint32_t n, hipStream_t str
         if (tiles > 0x7fffffffull) return hipErrorInvalidValue;
         if (tiles) {
             hipLaunchKernelGGL(block_slope, dim3((uint32_t)tiles), dim3(256), 0, stream, a);
-            if (launches) *launches += 1;
-        }
-        const uint64_t sums = fill_group(a, p + at, count, [](const SlopeProblem &q) { return q.db && q.M > kSlopeRows ? (uint64_t)(q.N + 63) / 64 : 0; });
-        if (sums) {
-            hipLaunchKernelGGL(block_column_sums, dim3((uint32_t)sums), dim3(256), 0, stream, a);
             if (launches) *launches += 1;
         }
         const hipError_t e = hipGetLastError();

@@ -233,7 +233,7 @@ struct Fragments {
 //   uint32_t tiles(); Place place(id); Operand m(Place), n(Place);
 //   begin(Place, Held, m, n, lane): before the first multiply; (m, n) is the wavefront's corner in the tile;
 //   finish(Place, acc, Held, m, n, lane, landed): calls landed() before its first store.
-// Place has m0, n0 and depth.  The grid has at most tiles() workgroups.
+// Place has m0, n0 and depth.  Workgroups begin at tiles of their own, below tiles(), and go on by `stride`, as many as there are workgroups.
 template <int BM, int BN, int WM, int WN, bool TRM, bool TRN, bool PAIRS = false>
 struct TileMfma {
     static constexpr int kWavesT = WM * WN, kThreads = 64 * kWavesT;
@@ -247,7 +247,7 @@ struct TileMfma {
     typedef f32x16 Acc[FN][FM];
 
     template <typename Walk>
-    __device__ static void run(const Walk &walk, unsigned char *smem)
+    __device__ static void run(const Walk &walk, unsigned char *smem, uint32_t begin = blockIdx.x, uint32_t stride = gridDim.x)
     {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -259,7 +259,7 @@ struct TileMfma {
         fn.init(wn * (32u * FN), lane);
 
         const uint32_t tiles = walk.tiles();
-        uint32_t id = blockIdx.x;                // of the tile that the streams walk towards
+        uint32_t id = begin;                // of the tile that the streams walk towards
         typename Walk::Place ahead = walk.place(id), cur = ahead;
         uint32_t cur_id = id;
         SM sm;
@@ -271,7 +271,7 @@ struct TileMfma {
         auto advance_m = [&]() {                 // the M side comes to the end of a tile first (or together with the N side)
             sm.advance();
             if (sm.slabs_left != 0) return;
-            id += gridDim.x;
+            id += stride;
             if (id < tiles) {
                 ahead = walk.place(id);
                 sm.locate(walk.m(ahead), ahead.m0, wave);
@@ -384,7 +384,7 @@ struct TileMfma {
                 if (!landed) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 landed = true;
             });
-            cur_id += gridDim.x;
+            cur_id += stride;
             if (cur_id >= tiles) {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may arrive in LDS after this workgroup
                 break;
@@ -411,7 +411,7 @@ struct TilePair {
     typedef f32x16 Acc[FN][FM];
 
     template <typename Walk>
-    __device__ static void run(const Walk &walk, unsigned char *smem)
+    __device__ static void run(const Walk &walk, unsigned char *smem, uint32_t begin = blockIdx.x, uint32_t stride = gridDim.x)
     {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -423,7 +423,7 @@ struct TilePair {
         fn.init(wn * (32u * FN), lane);
 
         const uint32_t tiles = walk.tiles();
-        uint32_t id = blockIdx.x;                // of the tile that the M stream walks towards
+        uint32_t id = begin;                // of the tile that the M stream walks towards
         typename Walk::Place ahead = walk.place(id), cur = ahead;
         uint32_t cur_id = id;
         SM sm;
@@ -435,7 +435,7 @@ struct TilePair {
         // Crossed into right before the first request of the next tile, the M side first (k-step 3 of the last but one slab).
         auto cross_m = [&]() {
             if (sm.slabs_left != 0) return;
-            id += gridDim.x;
+            id += stride;
             if (id < tiles) {
                 ahead = walk.place(id);
                 sm.locate(walk.m(ahead), ahead.m0, wave);
@@ -535,7 +535,7 @@ struct TilePair {
                 if (!landed) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 landed = true;
             });
-            cur_id += gridDim.x;
+            cur_id += stride;
             if (cur_id >= tiles) {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may arrive in LDS after this workgroup
                 break;
@@ -562,7 +562,7 @@ struct TileStream {
     typedef f32x16 Acc[FN][FM];
 
     template <typename Walk>
-    __device__ static void run(const Walk &walk, unsigned char *smem)
+    __device__ static void run(const Walk &walk, unsigned char *smem, uint32_t begin = blockIdx.x, uint32_t stride = gridDim.x)
     {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -573,7 +573,7 @@ struct TileStream {
         fm.init(wm * (32u * FM), lane);
         fn.init(wn * (32u * FN), lane);
         const uint32_t tiles = walk.tiles();
-        uint32_t id = blockIdx.x, cur_id = id;
+        uint32_t id = begin, cur_id = id;
         typename Walk::Place ahead = walk.place(id), cur = ahead;
         SM sm;
         SN sn;
@@ -593,7 +593,7 @@ struct TileStream {
             sm.advance();
             sn.advance();
             if (sm.slabs_left != 0) return;
-            id += gridDim.x;
+            id += stride;
             if (id < tiles) {
                 ahead = walk.place(id);
                 sm.locate(walk.m(ahead), ahead.m0, wave);
@@ -654,7 +654,7 @@ struct TileStream {
 #pragma unroll
                     for (int r = 0; HALVES && r < 16; ++r) acc[0][j][i][r] += acc[kSums - 1][j][i][r];
             walk.finish(cur, acc[0], typename Walk::Held{}, wm * (32u * FM), wn * (32u * FN), fresh_lane(), []() {});
-            cur_id += gridDim.x;
+            cur_id += stride;
             if (cur_id >= tiles) {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may arrive in LDS after this workgroup
                 break;
@@ -680,7 +680,7 @@ struct TileRows {
     typedef f32x16 Acc[FN][FM];
 
     template <typename Walk>
-    __device__ static void run(const Walk &walk, unsigned char *smem)
+    __device__ static void run(const Walk &walk, unsigned char *smem, uint32_t begin = blockIdx.x, uint32_t stride = gridDim.x)
     {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -692,7 +692,7 @@ struct TileRows {
         fn.init(wn * (32u * FN), lane);
 
         const uint32_t tiles = walk.tiles();
-        uint32_t id = blockIdx.x;                // of the tile that the M stream walks towards
+        uint32_t id = begin;                // of the tile that the M stream walks towards
         typename Walk::Place ahead = walk.place(id), cur = ahead;
         uint32_t cur_id = id;
         SM sm;
@@ -705,7 +705,7 @@ struct TileRows {
         auto advance_m = [&]() {
             sm.advance();
             if (sm.slabs_left != 0) return;
-            id += gridDim.x;
+            id += stride;
             if (id < tiles) {
                 ahead = walk.place(id);
                 sm.locate(walk.m(ahead), ahead.m0, wave);
@@ -793,7 +793,7 @@ struct TileRows {
                 if (!landed) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 landed = true;
             });
-            cur_id += gridDim.x;
+            cur_id += stride;
             if (cur_id >= tiles) {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may arrive in LDS after this workgroup
                 break;
