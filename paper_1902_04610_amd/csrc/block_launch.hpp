@@ -20,13 +20,14 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 2) void block_stream(BlockA
 }
 
 // Large tiles (TileMfma, TilePair, TileRows): where a weight is used by 128 rows and more, or comes in whole rounds of tiles.
-template <int BM, int BN, int WM, int WN, Epilogue E>
+// ONCE (128 x 256): weights that one row tile uses and that come from HBM are asked for non-temporally.
+template <int BM, int BN, int WM, int WN, Epilogue E, bool ONCE = false>
 __global__ __launch_bounds__(64 * WM * WN, 2) void block_tiled(BlockArgs a)
 {
     using Walk = BlockWalk<BM, BN, E>;
     constexpr bool kPairs = E == Epilogue::kGated;
     using T = std::conditional_t<Walk::kTransposed, TileRows<BM, BN, WM, WN>,
-                                 std::conditional_t<BM * BN == 128 * 256, TilePair<BM, BN, WM, WN, false, kPairs>, TileMfma<BM, BN, WM, WN, false, true, kPairs>>>;
+                                 std::conditional_t<BM * BN == 128 * 256, TilePair<BM, BN, WM, WN, ONCE, kPairs>, TileMfma<BM, BN, WM, WN, false, true, kPairs>>>;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[T::kLds];
     const Walk walk(a);
     T::run(walk, smem);
@@ -64,7 +65,11 @@ struct Round {
 struct Tiling {
     uint32_t bm, cols, per_cu, above, upto, fixed, slab, rest;
     hipError_t (*launch)(const Round &);
+    bool once = false;       // asks for weights non-temporally: for weights from HBM and calls that do not need them again
 };
+// Bytes per nanosecond, of weights from HBM, the most that tiles of fewer than 64 rows, other tiles, and tiles that ask non-temporally reached over the launches of more than 224 MB of weights.
+// 32 jobs x 1 - 32 rows, gated 1000 -> 2760 and dense 2760 -> 1000 (530 MB): 128-row tiles non-temporal / cached 111 / 120 us.
+constexpr uint64_t kStreamNarrow = 4300, kStream = 4800, kStreamOnce = 5200;
 constexpr uint32_t kAnyRows = ~0u;
 
 inline uint64_t launch_ns(const Tiling &t, const BlockProblem *p, uint32_t n)
@@ -83,15 +88,23 @@ inline uint64_t launch_ns(const Tiling &t, const BlockProblem *p, uint32_t n)
 }
 
 struct Choice { const Tiling *tiling; uint64_t ns; };
+// cached: as for launch_grouped_bf16; else no tiling is quicker than the weights' stream.  column_bytes: of a weight's row per output column.
 template <size_t N>
-inline Choice choose(const Tiling (&tilings)[N], const BlockProblem *p, uint32_t n)
+inline Choice choose(const Tiling (&tilings)[N], const BlockProblem *p, uint32_t n, bool cached, uint32_t column_bytes = 2)
 {
     uint32_t rows = 0;
-    for (uint32_t i = 0; i < n; ++i) rows = std::max(rows, p[i].M);
+    uint64_t bytes = 0;
+    bool kept = false;       // for a backward pass, which reads the weights again
+    for (uint32_t i = 0; i < n; ++i) {
+        rows = std::max(rows, p[i].M);
+        bytes += (uint64_t)column_bytes * p[i].K * p[i].N;
+        kept = kept || p[i].Z;
+    }
     Choice best{nullptr, ~0ull};
     for (const Tiling &t : tilings) {
-        if (rows <= t.above || rows > t.upto) continue;
-        const uint64_t ns = launch_ns(t, p, n);
+        if (rows <= t.above || rows > t.upto || (t.once && (cached || kept))) continue;
+        uint64_t ns = launch_ns(t, p, n);
+        if (!cached) ns = std::max(ns, bytes / (t.once ? kStreamOnce : t.bm < 64 ? kStreamNarrow : kStream));
         if (ns < best.ns) best = {&t, ns};
     }
     return best;
@@ -102,10 +115,10 @@ inline hipError_t ring(const Round &r)
 {
     return launch_block<BlockArgs>(block_stream<BM, BN, WM, WN, D, E>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, 2 * resident_grid(), r.p, r.n, r.stream, r.launches);
 }
-template <int BM, int BN, int WM, int WN, int PER_CU, Epilogue E>
+template <int BM, int BN, int WM, int WN, int PER_CU, Epilogue E, bool ONCE = false>
 inline hipError_t tiled(const Round &r)
 {
-    return launch_block<BlockArgs>(block_tiled<BM, BN, WM, WN, E>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, PER_CU * resident_grid(), r.p, r.n, r.stream, r.launches);
+    return launch_block<BlockArgs>(block_tiled<BM, BN, WM, WN, E, ONCE>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, PER_CU * resident_grid(), r.p, r.n, r.stream, r.launches);
 }
 
 }  // namespace salus

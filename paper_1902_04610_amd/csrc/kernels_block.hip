@@ -165,6 +165,7 @@ constexpr Tiling kDense[] = {
     {64, 64, 2, 0, kAnyRows, 2400, 471, 2510, ring<64, 64, 2, 2, 4, Epilogue::kDense>},
     {128, 128, 2, 0, kAnyRows, 2900, 923, 6250, tiled<128, 128, 2, 2, 2, Epilogue::kDense>},
     {128, 256, 2, 0, kAnyRows, 2900, 1439, 10780, tiled<128, 256, 1, 4, 2, Epilogue::kDense>},
+    {128, 256, 2, 0, 128, 2900, 1340, 10000, tiled<128, 256, 1, 4, 2, Epilogue::kDense, true>, true},
     {256, 256, 1, 0, kAnyRows, 0, 1180, 11130, tiled<256, 256, 2, 4, 1, Epilogue::kDense>},
 };
 constexpr Tiling kGated[] = {      // half of a tile's columns are the gate's
@@ -175,6 +176,7 @@ constexpr Tiling kGated[] = {      // half of a tile's columns are the gate's
     {64, 64, 2, 0, kAnyRows, 2400, 806, 2280, ring<64, 128, 2, 2, 3, Epilogue::kGated>},
     {128, 64, 2, 0, kAnyRows, 2400, 1036, 3920, tiled<128, 128, 2, 2, 2, Epilogue::kGated>},
     {128, 128, 2, 0, kAnyRows, 1400, 1471, 8870, tiled<128, 256, 1, 4, 2, Epilogue::kGated>},
+    {128, 128, 2, 0, 128, 1400, 1370, 8300, tiled<128, 256, 1, 4, 2, Epilogue::kGated, true>, true},
     {256, 128, 1, 0, kAnyRows, 800, 1259, 8090, tiled<256, 256, 2, 4, 1, Epilogue::kGated>},
 };
 constexpr Tiling kGateGrad[] = {
@@ -187,19 +189,19 @@ constexpr Tiling kGateGrad[] = {
     {128, 128, 2, 0, kAnyRows, 0, 904, 14890, tiled<128, 128, 2, 2, 2, Epilogue::kGateGrad>},
     {256, 256, 1, 0, kAnyRows, 0, 1074, 19050, tiled<256, 256, 2, 4, 1, Epilogue::kGateGrad>},
 };
-hipError_t launch_block_dense(const BlockProblem *p, uint32_t n, bool, hipStream_t stream, uint64_t *launches)
+hipError_t launch_block_dense(const BlockProblem *p, uint32_t n, bool cached, hipStream_t stream, uint64_t *launches)
 {
-    return choose(kDense, p, n).tiling->launch({p, n, stream, launches});
+    return choose(kDense, p, n, cached).tiling->launch({p, n, stream, launches});
 }
 
-hipError_t launch_block_gated(const BlockProblem *p, uint32_t n, bool, hipStream_t stream, uint64_t *launches)
+hipError_t launch_block_gated(const BlockProblem *p, uint32_t n, bool cached, hipStream_t stream, uint64_t *launches)
 {
-    return choose(kGated, p, n).tiling->launch({p, n, stream, launches});
+    return choose(kGated, p, n, cached, 4).tiling->launch({p, n, stream, launches});
 }
 
-hipError_t launch_block_gate_grad(const BlockProblem *p, uint32_t n, bool, hipStream_t stream, uint64_t *launches)
+hipError_t launch_block_gate_grad(const BlockProblem *p, uint32_t n, bool cached, hipStream_t stream, uint64_t *launches)
 {
-    return choose(kGateGrad, p, n).tiling->launch({p, n, stream, launches});
+    return choose(kGateGrad, p, n, cached).tiling->launch({p, n, stream, launches});
 }
 
 // ---- slope of a dense layer -----------------------------------------------------------------------------------------------------

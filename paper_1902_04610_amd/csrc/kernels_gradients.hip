@@ -277,7 +277,7 @@ static hipError_t launch_few_rows(const WeightGradProblem *p, uint32_t n, hipStr
 
 // A launch of tiles of `side` x `side`, per_cu at a time on a compute unit, in nanoseconds (Tiling in kernels_block.hip says how).
 struct WeightTiling { uint32_t side, per_cu, fixed, slab, rest; };
-constexpr WeightTiling kWeight128 = {128, 2, 2400, 1062, 2380}, kWeight256 = {256, 1, 0, 1282, 6660};
+constexpr WeightTiling kWeight128 = {128, 2, 2400, 1062, 2380}, kWeight256 = {256, 1, 0, 1500, 7500};
 static uint64_t tiled_ns(const WeightGradProblem *p, uint32_t n, const WeightTiling &t)
 {
     const uint64_t side = t.side, per_cu = t.per_cu, fixed = t.fixed, slab = t.slab, rest = t.rest;
@@ -331,8 +331,8 @@ static hipError_t launch_weight_grad(const WeightGradProblem *p, uint32_t n, hip
 static hipError_t launch_input_grad(const BlockProblem *p, uint32_t n, bool cached, hipStream_t stream, uint64_t *launches)
 {
     if (n == 0) return hipSuccess;
-    const Choice large = choose(kInputLarge, p, n);
-    if (large.ns < choose(kInputOther, p, n).ns) return large.tiling->launch({p, n, stream, launches});
+    const Choice large = choose(kInputLarge, p, n, true);
+    if (large.ns < choose(kInputOther, p, n, true).ns) return large.tiling->launch({p, n, stream, launches});
     std::vector<Problem> q;
     q.reserve(n);
     for (uint32_t i = 0; i < n; ++i) q.push_back({p[i].W, p[i].X, p[i].Y, nullptr, p[i].M, p[i].K, p[i].N, kOutBf16});
@@ -356,7 +356,8 @@ static hipError_t launch_sums(const SlopeProblem *p, uint32_t n, hipStream_t str
 }
 
 // Do input and weight gradients share a launch of 128 x 128 tiles?  Its time, from the tiles' as they run two on a compute unit: the longest tile, or all of them over all places and a quarter of
-// the longest for the end; against the quickest launches of their own and 1.2 us for each that is saved (a launch that adds columns: 3.5).  43 training calls of drawn sizes: 0.97 of the time if
+// the longest for the end, of which a sixteenth is taken off: they measured that much quicker than this says; against the quickest launches of their own and 1.2 us for each that is saved (a launch
+// that adds columns: 3.5).  Training calls of drawn sizes: 0.90 of the time where this shares; over 43 of them 0.97 if
 // always shared, with 0.66 - 1.47 at the ends: 5 jobs x 125 - 262 rows, 704 -> 112, 18.9 / 28.4 us, 1 job x 486 rows, depth 14224, whose few input gradient tiles one compute unit walks alone,
 // 197 / 134.  4 jobs x 500 rows, 2048 -> 2048: 48.5, alone 4.6 + 22.2 + 23.4.
 static bool share_tiled(const BlockProblem *input, uint32_t n_input, const WeightGradProblem *weight, uint32_t n_weight, bool sums)
@@ -374,9 +375,9 @@ static bool share_tiled(const BlockProblem *input, uint32_t n_input, const Weigh
     const uint64_t cus = resident_grid();
     if (tiles <= cus) longest = longest * 6 / 10;
     const uint64_t shared = 2000 + std::max(longest, work / (2 * cus) + longest / 4);
-    const uint64_t alone = std::min(choose(kInputLarge, input, n_input).ns, choose(kInputOther, input, n_input).ns) +
+    const uint64_t alone = std::min(choose(kInputLarge, input, n_input, true).ns, choose(kInputOther, input, n_input, true).ns) +
                            std::min(tiled_ns(weight, n_weight, kWeight128), tiled_ns(weight, n_weight, kWeight256));
-    return shared < alone + 1200 + (sums ? 3500 : 0);
+    return shared - shared / 16 < alone + 1200 + (sums ? 3500 : 0);
 }
 
 // And a launch of ring tiles and register blocks?  Beside the writes an input gradient's tile takes up to twice as long: worth it unless that is what the launch lasts.  More than 16 rows: depth up to 4096, or any where
