@@ -1,0 +1,248 @@
+"""Rounds of transformer-block operators and the kernels that each takes (not a test module): test_block_dispatch.py records the
+launches on the CPU, test_gpu_block_rounds.py runs the same rounds against the oracle.
+
+A round is (kind, jobs, bytes that the pool holds besides, kernels: E0 dense, E1 gated, E2 gate gradient, E3 input gradient): jobs are (M, K, F, N) for "gated" and "gated_train", (M, K, N) for "dense" and
+"dense_train", tuples of element counts for "clip" and "clip_sgd"."""
+import json
+import os
+import re
+import subprocess
+import sys
+
+from paper_1902_04610_amd import build
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+PAST = 240 << 20                     # more than the memory-side cache keeps of a pool's weights
+
+
+def jobs(n, M, *widths):
+    """n jobs of M rows and fewer, the last width of every third 8 more."""
+    return [(M - 3 * i % (M // 3 + 1),) + widths[:-1] + (widths[-1] + 8 * (i % 3 == 2),) for i in range(n)]
+
+
+ROUNDS = [
+    ("gated", jobs(1, 1, 1024, 264, 1024), 0, [
+        "block_narrow<1, 2, false, true, BlockFewArgs>", "block_narrow<1, 1, false, false, BlockFewArgs>"]),
+    ("gated", jobs(16, 1, 72, 8, 4096), 0, [
+        "block_narrow<1, 2, false, true, BlockArgs>", "block_narrow<1, 4, true, false, BlockArgs>"]),
+    ("gated", jobs(16, 16, 8, 520, 128), 0, [
+        "block_narrow<1, 4, true, true, BlockArgs>", "block_narrow<1, 1, false, false, BlockArgs>"]),
+    ("gated", jobs(4, 16, 72, 1032, 72), 0, [
+        "block_narrow<1, 4, true, true, BlockFewArgs>", "block_narrow<1, 1, false, false, BlockFewArgs>"]),
+    ("gated", jobs(1, 20, 8, 64, 64), 0, [
+        "block_narrow<2, 2, false, true, BlockFewArgs>", "block_narrow<2, 1, false, false, BlockFewArgs>"]),
+    ("gated", jobs(2, 48, 8, 1024, 1032), 0, [
+        "block_narrow<2, 2, false, true, BlockFewArgs>", "block_narrow<2, 2, false, false, BlockFewArgs>"]),
+    ("gated", jobs(8, 20, 1000, 8, 1032), 0, [
+        "block_narrow<2, 2, false, true, BlockArgs>", "block_narrow<2, 4, true, false, BlockArgs>"]),
+    ("gated", jobs(1, 128, 8, 1032, 72), 0, [
+        "block_narrow<2, 4, true, true, BlockFewArgs>", "block_narrow<2, 1, false, false, BlockFewArgs>"]),
+    ("gated", jobs(4, 100, 8, 72, 1032), 0, [
+        "block_narrow<2, 2, false, true, BlockFewArgs>", "block_narrow<2, 4, true, false, BlockFewArgs>"]),
+    ("gated", jobs(16, 200, 72, 520, 64), 0, [
+        "block_stream<64, 128, 2, 2, 3, E1>", "block_narrow<2, 2, false, false, BlockArgs>"]),
+    ("gated", jobs(16, 256, 64, 1032, 72), 0, [
+        "block_tiled<256, 256, 2, 4, E1, false>", "block_narrow<2, 4, true, false, BlockArgs>"]),
+    ("gated", jobs(60, 200, 1032, 72, 1000), 0, [
+        "block_tiled<128, 128, 2, 2, E1, false>", "block_tiled<128, 128, 2, 2, E1, false>", "block_tiled<256, 256, 2, 4, E0, false>", "block_tiled<256, 256, 2, 4, E0, false>"]),
+    ("gated", jobs(4, 100, 64, 16384, 64), PAST, [
+        "block_tiled<128, 256, 1, 4, E1, true>", "block_narrow<2, 1, false, false, BlockFewArgs>"]),
+    ("gated", jobs(4, 128, 64, 16384, 64), PAST, [
+        "block_tiled<128, 256, 1, 4, E1, true>", "block_narrow<2, 1, false, false, BlockFewArgs>"]),
+    ("gated", jobs(4, 128, 64, 16384, 64), 0, [
+        "block_tiled<128, 256, 1, 4, E1, false>", "block_narrow<2, 1, false, false, BlockFewArgs>"]),
+    ("dense", jobs(16, 1, 8, 264), 0, [
+        "block_narrow<1, 2, false, false, BlockArgs>"]),
+    ("dense", jobs(4, 16, 1032, 2048), 0, [
+        "block_narrow<1, 4, true, false, BlockFewArgs>"]),
+    ("dense", jobs(4, 1, 264, 4096), 0, [
+        "block_narrow<1, 4, true, false, BlockFewArgs>"]),
+    ("dense", jobs(8, 100, 72, 8), 0, [
+        "block_narrow<2, 1, false, false, BlockArgs>"]),
+    ("dense", jobs(1, 33, 1000, 520), 0, [
+        "block_narrow<2, 1, false, false, BlockFewArgs>"]),
+    ("dense", jobs(4, 64, 520, 1032), 0, [
+        "block_narrow<2, 4, true, false, BlockFewArgs>"]),
+    ("dense", jobs(2, 128, 264, 4096), 0, [
+        "block_stream<64, 64, 2, 2, 4, E0>"]),
+    ("dense", jobs(40, 64, 520, 520), 0, [
+        "block_stream<64, 64, 2, 2, 4, E0>"]),
+    ("dense", jobs(2, 1000, 264, 4096), 0, [
+        "block_tiled<128, 256, 1, 4, E0, false>"]),
+    ("dense", jobs(4, 128, 64, 32768), PAST, [
+        "block_tiled<128, 256, 1, 4, E0, true>"]),
+    ("dense", jobs(4, 128, 64, 32768), 0, [
+        "block_tiled<128, 128, 2, 2, E0, false>"]),
+    ("dense", jobs(2, 2000, 264, 4096), 0, [
+        "block_tiled<256, 256, 2, 4, E0, false>"]),
+    ("dense", jobs(60, 128, 72, 264), 0, [
+        "block_tiled<128, 128, 2, 2, E0, false>", "block_tiled<128, 128, 2, 2, E0, false>"]),
+    ("dense", jobs(2, 16, 264, 4096), 0, [
+        "block_narrow<1, 2, false, false, BlockFewArgs>"]),
+    ("gated_train", jobs(1, 1, 8, 8, 1024), 0, [
+        "block_narrow<1, 2, false, true, BlockFewArgs>", "block_narrow<1, 1, false, false, BlockFewArgs>", "block_gate_grad_narrow<1, 2, BlockFewArgs>", "gradients_few_rows"]),
+    ("gated_train", jobs(8, 5, 64, 128, 1000), 0, [
+        "block_narrow<1, 2, false, true, BlockArgs>", "block_narrow<1, 2, false, false, BlockArgs>", "block_gate_grad_narrow<1, 2, BlockArgs>", "gradients_few_rows"]),
+    ("gated_train", jobs(40, 16, 8, 264, 1000), 0, [
+        "block_narrow<1, 4, true, true, BlockArgs>", "block_narrow<1, 4, true, false, BlockArgs>", "block_gate_grad_narrow<1, 4, BlockArgs>", "grouped_dense_bf16_narrow<1, true, 2, 8, true>", "weight_grad_few_rows", "weight_grad_few_rows"]),
+    ("gated_train", jobs(4, 16, 8, 8192, 64), 0, [
+        "block_stream<64, 128, 2, 2, 3, E1>", "block_narrow<1, 1, false, false, BlockFewArgs>", "block_gate_grad_narrow<1, 4, BlockFewArgs>", "grouped_dense_bf16_narrow<1, true, 2, 8, true>", "weight_grad_few_rows"]),
+    ("gated_train", jobs(16, 48, 128, 8, 8), 0, [
+        "block_narrow<2, 2, false, true, BlockArgs>", "block_narrow<2, 1, false, false, BlockArgs>", "block_gate_grad_narrow<2, 2, BlockArgs>", "gradients_few_rows"]),
+    ("gated_train", jobs(1, 64, 8, 72, 64), 0, [
+        "block_narrow<2, 2, false, true, BlockFewArgs>", "block_narrow<2, 1, false, false, BlockFewArgs>", "block_gate_grad_narrow<2, 2, BlockFewArgs>", "gradients_few_rows"]),
+    ("gated_train", jobs(8, 128, 8, 264, 264), 0, [
+        "block_narrow<2, 4, true, true, BlockArgs>", "block_narrow<2, 4, true, false, BlockArgs>", "block_gate_grad_narrow<2, 4, BlockArgs>", "gradients_tiled"]),
+    ("gated_train", jobs(2, 200, 64, 1000, 520), 0, [
+        "block_narrow<2, 4, true, true, BlockFewArgs>", "block_narrow<2, 2, false, false, BlockFewArgs>", "block_gate_grad_narrow<2, 4, BlockFewArgs>", "grouped_dense_bf16_narrow<2, true, 2, 8, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
+    ("gated_train", jobs(4, 128, 8, 1032, 8), 0, [
+        "block_stream<64, 128, 2, 2, 3, E1>", "block_narrow<2, 1, false, false, BlockFewArgs>", "block_stream<64, 64, 2, 2, 4, E2>", "grouped_dense_bf16_narrow<2, true, 2, 8, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
+    ("gated_train", jobs(8, 500, 8, 264, 8), 0, [
+        "block_tiled<128, 128, 2, 2, E1, false>", "block_narrow<2, 1, false, false, BlockArgs>", "block_stream<64, 128, 2, 2, 3, E2>", "gradients_tiled"]),
+    ("gated_train", jobs(60, 100, 8, 2048, 128), 0, [
+        "block_tiled<128, 256, 1, 4, E1, false>", "block_tiled<128, 256, 1, 4, E1, false>", "block_narrow<2, 4, true, false, BlockArgs>", "block_narrow<2, 4, true, false, BlockArgs>", "block_tiled<128, 128, 2, 2, E2, false>", "block_tiled<128, 128, 2, 2, E2, false>", "grouped_dense_bf16_narrow<2, true, 2, 8, false>", "weight_grad_few_rows", "weight_grad_few_rows"]),
+    ("gated_train", jobs(1, 2048, 8, 8192, 8), 0, [
+        "block_tiled<256, 256, 2, 4, E1, false>", "block_narrow<2, 1, false, false, BlockFewArgs>", "block_tiled<256, 256, 2, 4, E2, false>", "grouped_dense_bf16_narrow<2, true, 2, 8, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
+    ("gated_train", jobs(4, 300, 520, 264, 264), 0, [
+        "block_narrow<2, 4, true, true, BlockFewArgs>", "block_narrow<2, 4, true, false, BlockFewArgs>", "block_gate_grad_narrow<2, 4, BlockFewArgs>", "gradients_tiled"]),
+    ("dense_train", jobs(1, 16, 8, 8), 0, [
+        "block_narrow<1, 1, false, false, BlockFewArgs>", "block_slope", "gradients_few_rows"]),
+    ("dense_train", jobs(40, 20, 64, 64), 0, [
+        "block_narrow<2, 1, false, false, BlockArgs>", "block_slope", "block_column_sums", "grouped_dense_bf16_narrow<2, true, 2, 8, true>", "weight_grad_few_rows"]),
+    ("dense_train", jobs(40, 16, 520, 72), 0, [
+        "block_narrow<1, 1, false, false, BlockArgs>", "block_slope", "grouped_dense_bf16<1, true, true>", "weight_grad_few_rows"]),
+    ("dense_train", jobs(40, 5, 8, 64), 0, [
+        "block_narrow<1, 1, false, false, BlockArgs>", "block_slope", "grouped_dense_bf16_narrow<1, true, 2, 8, true>", "weight_grad_few_rows"]),
+    ("dense_train", jobs(40, 200, 264, 72), 0, [
+        "block_stream<64, 64, 2, 2, 4, E0>", "block_slope", "block_column_sums", "block_column_sums", "block_tiled<128, 128, 2, 2, E3, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
+    ("dense_train", jobs(1, 256, 8, 8), 0, [
+        "block_narrow<2, 1, false, false, BlockFewArgs>", "block_slope", "gradients_tiled"]),
+    ("dense_train", jobs(60, 500, 8, 8), 0, [
+        "block_stream<64, 64, 2, 2, 4, E0>", "block_stream<64, 64, 2, 2, 4, E0>", "block_slope", "block_slope", "block_column_sums", "block_column_sums", "grouped_dense_bf16_stream<64, 128, 2, 2, 1, true, 3>", "weight_grad_tiled<128, 128, 2, 2>"]),
+    ("dense_train", jobs(60, 48, 128, 8), 0, [
+        "block_narrow<2, 1, false, false, BlockArgs>", "block_narrow<2, 1, false, false, BlockArgs>", "block_slope", "block_slope", "block_column_sums", "block_column_sums", "grouped_dense_bf16_narrow<2, true, 2, 8, true>", "grouped_dense_bf16_stream<64, 64, 2, 1, 2, true, 4>", "weight_grad_few_rows"]),
+    ("dense_train", jobs(8, 97, 264, 520), 0, [
+        "block_narrow<2, 4, true, false, BlockArgs>", "block_slope", "gradients_few_rows"]),
+    ("dense_train", jobs(8, 90, 264, 520), 0, [
+        "block_narrow<2, 4, true, false, BlockArgs>", "block_slope", "gradients_few_rows"]),
+    ("dense_train", jobs(1, 16, 1032, 4096), 0, [
+        "block_narrow<1, 1, false, false, BlockFewArgs>", "block_slope", "grouped_dense_bf16_narrow<1, true, 2, 8, true>", "weight_grad_few_rows"]),
+    ("dense_train", jobs(1, 24, 1032, 4096), 0, [
+        "block_narrow<2, 1, false, false, BlockFewArgs>", "block_slope", "gradients_few_rows"]),
+    ("dense_train", jobs(4, 300, 520, 520), 0, [
+        "block_stream<64, 64, 2, 2, 4, E0>", "block_slope", "gradients_tiled"]),
+    ("dense_train", jobs(1, 150, 4096, 4096), 0, [
+        "block_stream<64, 64, 2, 2, 4, E0>", "block_slope", "block_column_sums", "grouped_dense_bf16_stream<64, 64, 2, 1, 2, true, 4>", "weight_grad_tiled<256, 256, 2, 4>"]),
+    ("dense_train", jobs(1, 4001, 4088, 520), 0, [
+        "block_tiled<128, 128, 2, 2, E0, false>", "block_slope", "block_column_sums", "block_tiled<256, 256, 2, 4, E3, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
+    ("clip", [(100, 9)] * 3, 0, [
+        "clip_norm<ClipArgsOf<16u, 4u> >", "clip_apply<false, false, ClipArgsOf<16u, 4u> >"]),
+    ("clip", [(100, 9)] * 5, 0, [
+        "clip_norm<ClipArgsOf<64u, 32u> >", "clip_apply<false, false, ClipArgsOf<64u, 32u> >"]),
+    ("clip", [(125829120,)], 0, [
+        "clip_norm<ClipArgsOf<16u, 4u> >", "clip_apply<false, true, ClipArgsOf<16u, 4u> >"]),
+    ("clip", [(31457280,)] * 5, 0, [
+        "clip_norm<ClipArgsOf<64u, 32u> >", "clip_apply<false, true, ClipArgsOf<64u, 32u> >"]),
+    ("clip_sgd", [(100,)] * 4, 0, [
+        "clip_norm<ClipArgsOf<16u, 4u> >", "clip_apply<true, false, ClipArgsOf<16u, 4u> >"]),
+    ("clip_sgd", [(100,)] * 40, 0, [
+        "clip_norm<ClipArgsOf<64u, 32u> >", "clip_norm<ClipArgsOf<64u, 32u> >", "clip_apply<true, false, ClipArgsOf<64u, 32u> >", "clip_apply<true, false, ClipArgsOf<64u, 32u> >"]),
+    ("clip_sgd", [(31457280, 9)], 0, [
+        "clip_norm<ClipArgsOf<16u, 4u> >", "clip_apply<true, true, ClipArgsOf<16u, 4u> >"]),
+    ("clip_sgd", [(8388608,)] * 5, 0, [
+        "clip_norm<ClipArgsOf<64u, 32u> >", "clip_apply<true, true, ClipArgsOf<64u, 32u> >"]),
+]
+
+CHILD = r"""
+import ctypes, json, sys
+from paper_1902_04610_amd import salus as s
+take = ctypes.CDLL(None).recorder_take
+take.restype = ctypes.c_char_p
+up = lambda v: (v + 255) // 256 * 256
+
+def place(sizes):
+    at, out = 0, {}
+    for name, n in sizes:
+        out[name + "_off"] = at
+        at += up(n)
+    return out, max(at, 256)
+
+def parts(kind, size):
+    train = kind.endswith("_train")
+    if kind.startswith("gated"):
+        M, K, F, N = size
+        p = [("w_in", K * 2 * F * 2), ("w_out", F * N * 2)]
+        l = [("x", M * K * 2), ("r", M * N * 2), ("y", M * N * 2), ("h", M * F * 2)]
+        if train:
+            l += [("gu", M * 2 * F * 4), ("dy", M * N * 2), ("dx", M * K * 2), ("dw_in", K * 2 * F * 2), ("dw_out", F * N * 2), ("work", s.gated_grad_work_bytes(M, F))]
+        return p, l, dict(M=M, K=K, F=F, N=N, act=s.ACT_SILU)
+    M, K, N = size
+    p = [("w", K * N * 2), ("b", N * 2)]
+    l = [("x", M * K * 2), ("r", M * N * 2), ("y", M * N * 2)]
+    if train:
+        l += [("z", M * N * 4), ("dy", M * N * 2), ("dx", M * K * 2), ("dw", K * N * 2), ("db", N * 4), ("work", s.dense_grad_work_bytes(M, N))]
+    return p, l, dict(M=M, K=K, N=N, act=s.ACT_GELU, y_dtype=s.BF16)
+
+def run(kind, jobs, idle):
+    built = []
+    for size in jobs:
+        if kind.startswith("clip"):
+            tensors, at, pt = [], 0, 0
+            for n in size:
+                t = dict(count=n, dtype=s.BF16, g_off=at)
+                at += up(2 * n)
+                if kind == "clip_sgd":
+                    t.update(wm_off=pt, wb_off=pt + up(4 * n))
+                    pt += up(4 * n) + up(2 * n)
+                tensors.append(t)
+            built.append((max(pt, 256), at + 256 + up(s.clip_work_bytes(tensors)), dict(tensors=tensors, max_norm=1.0, lr=0.1, norm_off=at, work_off=at + 256)))
+            continue
+        p, l, item = parts(kind, size)
+        p, P = place(p)
+        l, E = place(l)
+        built.append((P, E, dict(item, **p, **l)))
+    pool = s.Pool(1 << 40, sum(P + E for P, E, _ in built) + up(idle) + 4096, stream=0x50, policy=s.POLICY_PACK)
+    if idle:
+        assert pool.lane_alloc(up(idle), 256, 0, 0)[0] == s.OK
+    items = []
+    for P, E, item in built:
+        status, job = pool.lane_alloc(P, E, 0, 0)
+        assert status == s.OK
+        items.append(dict(item, job=job))
+    def call(make, run, fields=None):
+        descs, keep = make([{k: v for k, v in i.items() if fields is None or k in fields} for i in items])
+        take()
+        assert run(descs, stream=0x50) == s.OK, pool.last_error()
+        return take().decode()
+    size = "job M K F N act "
+    names = lambda v: (size + " ".join(n if n == "y_dtype" else n + "_off" for n in v.split())).split()
+    if kind.startswith("gated"):
+        out = call(pool.make_gated_descs, pool.grouped_gated_forward, names("w_in w_out x y h r gu"))
+        if kind == "gated_train":
+            out += call(pool.make_gated_grad_descs, pool.grouped_gated_backward, names("w_in w_out x h gu dy dx dw_in dw_out work"))
+    elif kind.startswith("dense"):
+        out = call(pool.make_dense_descs, pool.grouped_dense_forward, names("y_dtype w b x y r z"))
+        if kind == "dense_train":
+            out += call(pool.make_dense_grad_descs, pool.grouped_dense_backward, names("w x z dy dx dw db work"))
+    else:
+        out = call(pool.make_clip_descs, pool.grouped_clip if kind == "clip" else pool.grouped_clip_sgd)
+    pool.close()
+    return out
+
+print(json.dumps([run(*c) for c in json.load(sys.stdin)]))
+"""
+
+
+def kernels(rounds, tmp):
+    """The kernels that each round launches, in order, with their template arguments."""
+    if not os.path.exists(build.LIB):
+        build.build()
+    so = os.path.join(str(tmp), "librecorder.so")
+    subprocess.check_call(["gcc", "-O1", "-fPIC", "-shared", "-Wall", "-o", so, os.path.join(HERE, "launch_recorder.c")])
+    env = dict(os.environ, LD_PRELOAD=":".join(filter(None, [so, os.environ.get("LD_PRELOAD")])), PYTHONPATH=build.ROOT)
+    r = subprocess.run([sys.executable, "-c", CHILD], input=json.dumps(rounds), cwd=build.ROOT, env=env, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    logs = "----\n".join(json.loads(r.stdout.splitlines()[-1]))
+    plain = subprocess.run(["c++filt"], input=logs, stdout=subprocess.PIPE, text=True, check=True).stdout
+    plain = re.sub(r"\((salus::)?Epilogue\)", "E", plain).replace("salus::", "").replace("(anonymous namespace)::", "").replace("void ", "")
+    return [re.findall(r"^launch (.+?)\([^()]*\) \d+ \d+ ", log, re.M) for log in plain.split("----\n")]
