@@ -335,7 +335,7 @@ int32_t salus_grouped_train_step(salus_pool_t *pool, const salus_train_desc *des
  * rules of salus_grouped_forward (pairwise different lanes, every buffer inside the
  * lane or the persistent block).  All matrices are row-major, inputs and weights bf16; sums
  * are float.  K, F and N are positive multiples of 8 below 2^22 (2 F as well), M
- * is at least 1; offsets are multiples of 16.  What is written may overlap nothing else of
+ * is at least 1 and below 2^31; offsets are multiples of 16.  What is written may overlap nothing else of
  * the job's call, except that y may be r itself where y is bf16 (a residual
  * stream updated in place); what is only read may coincide (x and r).  The calls
  * are plain kernel launches with by-value arguments and can be recorded in a graph;

@@ -62,9 +62,10 @@ int32_t guarded(F body)
 }
 
 bool width_ok(uint64_t w) { return w != 0 && w % 8 == 0 && w < kTiledMaxWidth; }
+bool rows_ok(uint32_t m) { return m != 0 && m < 1u << 31; }
 bool act_ok(int32_t act) { return act >= SALUS_ACT_NONE && act <= SALUS_ACT_SILU; }
 
-const char *const kWidths = "K, F and N must be positive multiples of 8 below 2^22 (2 F as well), M positive";
+const char *const kWidths = "K, F and N must be positive multiples of 8 below 2^22 (2 F as well), M positive and below 2^31";
 const char *const kAct = "bad activation";
 const char *const kWeights = "weights outside the persistent block";
 const char *const kLane = "buffer outside the job's lane";
@@ -98,7 +99,7 @@ int32_t gated_forward(salus_pool_t *pool, const salus_gated_desc *descs, uint32_
     in.reserve(n);
     out.reserve(n);
     const int32_t rc = for_jobs(pool, descs, n, [&](const salus_gated_desc &d, const Placed &at) -> const char * {
-        if (d.M == 0 || !width_ok(d.K) || !width_ok(2ull * d.F) || !width_ok(d.F) || !width_ok(d.N)) return kWidths;
+        if (!rows_ok(d.M) || !width_ok(d.K) || !width_ok(2ull * d.F) || !width_ok(d.F) || !width_ok(d.N)) return kWidths;
         if (!act_ok(d.act)) return kAct;
         const uint64_t M = d.M;
         Ranges weights(at.P), lane(at.lane_size);
@@ -133,7 +134,7 @@ int32_t gated_backward(salus_pool_t *pool, const salus_gated_grad_desc *descs, u
     input.reserve(n);
     weight.reserve(2 * n);
     const int32_t rc = for_jobs(pool, descs, n, [&](const salus_gated_grad_desc &d, const Placed &at) -> const char * {
-        if (d.M == 0 || !width_ok(d.K) || !width_ok(2ull * d.F) || !width_ok(d.F) || !width_ok(d.N)) return kWidths;
+        if (!rows_ok(d.M) || !width_ok(d.K) || !width_ok(2ull * d.F) || !width_ok(d.F) || !width_ok(d.N)) return kWidths;
         if (!act_ok(d.act)) return kAct;
         const uint64_t M = d.M;
         Ranges weights(at.P), lane(at.lane_size);
@@ -172,7 +173,7 @@ int32_t dense_forward(salus_pool_t *pool, const salus_dense_desc *descs, uint32_
     std::vector<BlockProblem> problems;
     problems.reserve(n);
     const int32_t rc = for_jobs(pool, descs, n, [&](const salus_dense_desc &d, const Placed &at) -> const char * {
-        if (d.M == 0 || !width_ok(d.K) || !width_ok(d.N)) return kWidths;
+        if (!rows_ok(d.M) || !width_ok(d.K) || !width_ok(d.N)) return kWidths;
         if (!act_ok(d.act)) return kAct;
         if (d.y_dtype != SALUS_F32 && d.y_dtype != SALUS_BF16) return "bad dtype";
         const uint64_t M = d.M;
@@ -203,7 +204,7 @@ int32_t dense_backward(salus_pool_t *pool, const salus_dense_grad_desc *descs, u
     input.reserve(n);
     weight.reserve(n);
     const int32_t rc = for_jobs(pool, descs, n, [&](const salus_dense_grad_desc &d, const Placed &at) -> const char * {
-        if (d.M == 0 || !width_ok(d.K) || !width_ok(d.N)) return kWidths;
+        if (!rows_ok(d.M) || !width_ok(d.K) || !width_ok(d.N)) return kWidths;
         if (!act_ok(d.act)) return kAct;
         const bool linear = d.act == SALUS_ACT_NONE;
         if (linear != (d.z_off == SALUS_ABSENT)) return "z is given exactly if there is an activation";

@@ -77,13 +77,13 @@ struct NarrowTile {
             } else w_off[i] = tile.n0 + col < N ? krow[i] * pitch + (first_col + col) * 2u + (strip && first_col + col >= 128u ? (K - 1) * 256u : 0u) : kOutside;
         }
         uint64_t w_base = (uint64_t)(uintptr_t)W + (strip ? (uint64_t)(tile.n0 & ~127u) * K * 2u : 0);
-        uint64_t x_base = (uint64_t)(uintptr_t)X;
+        uint64_t x_base = (uint64_t)(uintptr_t)X + (ZEROS ? (uint64_t)tile.m0 * K * 2u : 0);
         uint32_t x_off[MT];
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             // a row tile that the job does not have (its rows are never stored) reads the last one instead
             const uint32_t row = tile.m0 + 16u * t + c, tt = min((uint32_t)t, xtiles - 1);
-            if (ZEROS) x_off[t] = row < M ? row * K * 2u + 16u * g : kOutside;
+            if (ZEROS) x_off[t] = row < M ? (row - tile.m0) * K * 2u + 16u * g : kOutside;
             else x_off[t] = blocked_in ? tt * 1024u + 16u * lane : (row < M ? row : M - 1) * K * 2u + 16u * g;
         }
         const uint64_t w_step = (uint64_t)32u * pitch, x_step = blocked_in ? xtiles * 1024u : 64u;

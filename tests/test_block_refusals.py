@@ -90,6 +90,7 @@ for kind in CALLS:
         continue
     for name in [n for n in ("M", "K", "F", "N") if n in base]:
         out[kind, name + " 0"] = call(kind, [dict(base, **{name: 0})])
+        out[kind, name + " 2147483648"] = call(kind, [dict(base, **{name: 1 << 31})])
         out[kind, name + " 4294967288"] = call(kind, [dict(base, **{name: 4294967288})])
         if name != "M":
             out[kind, name + " 12"] = call(kind, [dict(base, **{name: 12})])
@@ -157,6 +158,7 @@ def test_messages_name_the_fault(outcomes):
     assert "lane" in outcomes["gated", "x_off far beyond"][1]
     assert "overlap" in outcomes["gated", "h in gu"][1]
     assert "multiples of 8" in outcomes["dense", "K 12"][1]
+    assert "2^31" in outcomes["dense_grad", "M 2147483648"][1] and "2^31" in outcomes["gated", "M 4294967288"][1]
     assert "activation" in outcomes["dense_grad", "act 4"][1]
     assert "max_norm" in outcomes["clip", "max_norm nan"][1]
     assert "resident" in outcomes["clip_sgd", "evicted"][1]
