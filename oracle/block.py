@@ -123,5 +123,5 @@ def clip(tensors, max_norm):
     """tensors: float64 arrays.  Returns (norm, coefficient)."""
     norm = np.sqrt(sum(float((t * t).sum()) for t in tensors))
     with np.errstate(divide="ignore", invalid="ignore"):
-        ratio = np.float64(max_norm) / np.float64(norm)
+        ratio = np.float64(1) if norm <= max_norm else np.float64(max_norm) / np.float64(norm)
     return norm, ratio if ratio < 1 or np.isnan(ratio) else 1.0

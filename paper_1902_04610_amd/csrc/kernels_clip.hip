@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kClipThreads) void clip_apply(Args a)
 {
     const ClipWalk<Args> walk(a);
     const ClipOwner &job = a.job[walk.job];
-    const double norm = clip_total(job), ratio = (double)job.max_norm / norm;
+    const double norm = clip_total(job), ratio = norm <= (double)job.max_norm ? 1.0 : (double)job.max_norm / norm;      // no limit: also an infinite norm is within it
     if (job.norm && walk.mine == 0 && threadIdx.x == 0) *(Global<float> *)job.norm = (float)norm;
     const float scale = (float)(ratio > 1.0 ? 1.0 : ratio);
     // nothing is scaled below the limit: x 1 would write back what is there

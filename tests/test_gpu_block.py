@@ -174,6 +174,17 @@ def test_clip_of_what_is_not_finite():
     rnd.close()
 
 
+def test_clip_without_a_limit_leaves_infinities():
+    rng = np.random.default_rng(10)
+    jobs = [bu.clip_job(rng, [40, 3000], ["f32", "bf16"], scale=5.0, max_norm=np.inf) for _ in range(2)]
+    jobs[0]["parts"][2]["g0"][3] = np.inf
+    jobs[1]["parts"][2]["g0"][3] = np.nan
+    rnd = bu.run_clip(jobs)
+    assert rnd.read(0, "norm")[0] == np.inf and all(np.array_equal(rnd.read(0, n), jobs[0]["parts"][2][n]) for n in ("g0", "g1"))
+    assert np.isnan(rnd.read(1, "norm")[0]) and np.isnan(rnd.read(1, "g0")).all()
+    rnd.close()
+
+
 def test_the_same_bits_every_time_and_on_another_stream():
     rng = np.random.default_rng(6)
     gated = [bu.gated_job(rng, m, 264, 136, 200, train=True) for m in (1, 40, 150)]
