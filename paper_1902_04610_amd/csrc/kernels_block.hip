@@ -155,6 +155,8 @@ static hipError_t narrow_grad(const Round &r)
 // average and 28, 33 and 34 % at most; the best single kind is 38 (64 x 64), 32 (64 x 128) and 25 % (32 x 32) off.  What each is for: narrow tiles fill the chip with few rows, the
 // ring streams weights past one or two row tiles, large tiles multiply.  1 job x 1 row, 4096 -> 1024: 16 columns 9.4 us, the ring 16; 32 jobs x 1 - 32 rows, 1000 -> 5520, 64 x 64 / 128 x 128 / 128 x 256
 // 75 / 73 / 73, 2760 -> 1000 37 / 37 / 55; 8 jobs x 64 rows, 2736 -> 1024, 32 x 64 / 64 x 64 20.7 / 25.8; 8 jobs x 1000 rows, 2048 -> 8192, 64 x 128 / 128 x 128 / 128 x 256 / 256 x 256 545 / 353 / 295 / 286.
+// One 128 x 128 tile per compute unit: eight wavefronts instead of four, 4 jobs x 500 rows, 2048 -> 2048, 27.5 / 29.2 us, 2 x 2000, 1024 -> 1024, 18.3 / 19.7, 0.95 over 10 drawn launches of 130 - 256
+// tiles (gated and gate gradients: 0.98 - 1.04, not there); its time is set as the same share of the other's.
 constexpr Tiling kDense[] = {
     {16, 16, 1, 0, 16, 1300, 92, 1370, narrow<1, 1, false, Epilogue::kDense>},
     {32, 16, 1, 16, kAnyRows, 1300, 152, 1480, narrow<2, 1, false, Epilogue::kDense>},
@@ -164,6 +166,7 @@ constexpr Tiling kDense[] = {
     {32, 64, 2, 16, kAnyRows, 1800, 378, 3280, narrow<2, 4, true, Epilogue::kDense>},
     {64, 64, 2, 0, kAnyRows, 2400, 471, 2510, ring<64, 64, 2, 2, 4, Epilogue::kDense>},
     {128, 128, 2, 0, kAnyRows, 2900, 923, 6250, tiled<128, 128, 2, 2, 2, Epilogue::kDense>},
+    {128, 128, 1, 0, kAnyRows, 2800, 532, 3600, tiled<128, 128, 2, 4, 1, Epilogue::kDense>},
     {128, 256, 2, 0, kAnyRows, 2900, 1439, 10780, tiled<128, 256, 1, 4, 2, Epilogue::kDense>},
     {128, 256, 2, 0, 128, 2900, 1340, 10000, tiled<128, 256, 1, 4, 2, Epilogue::kDense, true>, true},
     {256, 256, 1, 0, kAnyRows, 0, 1180, 11130, tiled<256, 256, 2, 4, 1, Epilogue::kDense>},

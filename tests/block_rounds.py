@@ -76,7 +76,7 @@ ROUNDS = [
     ("dense", jobs(2, 2000, 264, 4096), 0, [
         "block_tiled<256, 256, 2, 4, E0, false>"]),
     ("dense", jobs(60, 128, 72, 264), 0, [
-        "block_tiled<128, 128, 2, 2, E0, false>", "block_tiled<128, 128, 2, 2, E0, false>"]),
+        "block_tiled<128, 128, 2, 4, E0, false>", "block_tiled<128, 128, 2, 4, E0, false>"]),
     ("dense", jobs(2, 16, 264, 4096), 0, [
         "block_narrow<1, 2, false, false, BlockFewArgs>"]),
     ("gated_train", jobs(1, 1, 8, 8, 1024), 0, [
@@ -134,7 +134,7 @@ ROUNDS = [
     ("dense_train", jobs(1, 150, 4096, 4096), 0, [
         "block_stream<64, 64, 2, 2, 4, E0>", "block_slope", "block_column_sums", "grouped_dense_bf16_stream<64, 64, 2, 1, 2, true, 4>", "weight_grad_tiled<256, 256, 2, 4>"]),
     ("dense_train", jobs(1, 4001, 4088, 520), 0, [
-        "block_tiled<128, 128, 2, 2, E0, false>", "block_slope", "block_column_sums", "block_tiled<256, 256, 2, 4, E3, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
+        "block_tiled<128, 128, 2, 4, E0, false>", "block_slope", "block_column_sums", "block_tiled<256, 256, 2, 4, E3, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
     ("clip", [(100, 9)] * 3, 0, [
         "clip_norm<ClipArgsOf<16u, 4u> >", "clip_apply<false, false, ClipArgsOf<16u, 4u> >"]),
     ("clip", [(100, 9)] * 5, 0, [
