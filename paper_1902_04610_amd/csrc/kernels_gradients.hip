@@ -355,6 +355,23 @@ static hipError_t launch_sums(const SlopeProblem *p, uint32_t n, hipStream_t str
     return hipSuccess;
 }
 
+// Tiles of 128 x 128 of a shared launch, two on a compute unit: how many, their times together and the longest, in nanoseconds.
+struct SharedTiles { uint64_t tiles, work, longest; };
+static SharedTiles shared_tiles(const BlockProblem *input, uint32_t n_input, const WeightGradProblem *weight, uint32_t n_weight)
+{
+    const Tiling &x = kInputLarge[0];
+    SharedTiles s{};
+    auto add = [&](uint64_t count, uint32_t depth, uint64_t slab, uint64_t rest) {
+        const uint64_t ns = std::max((depth + kSlab - 1) / kSlab, kMinSlabs) * slab + rest;
+        s.tiles += count;
+        s.work += count * ns;
+        s.longest = std::max(s.longest, ns);
+    };
+    for (uint32_t i = 0; i < n_input; ++i) add((uint64_t)((input[i].M + 127) / 128) * ((input[i].N + 127) / 128), input[i].K, x.slab, x.rest);
+    for (uint32_t i = 0; i < n_weight; ++i) add((uint64_t)((weight[i].K + 127) / 128) * ((weight[i].N + 127) / 128), weight[i].M, kWeight128.slab, kWeight128.rest);
+    return s;
+}
+
 // Do input and weight gradients share a launch of 128 x 128 tiles?  Its time, from the tiles' as they run two on a compute unit: the longest tile, or all of them over all places and a quarter of
 // the longest for the end, of which a sixteenth is taken off: they measured that much quicker than this says; against the quickest launches of their own and 1.2 us for each that is saved (a launch
 // that adds columns: 3.5).  Training calls of drawn sizes: 0.90 of the time where this shares; over 43 of them 0.97 if
@@ -362,19 +379,11 @@ static hipError_t launch_sums(const SlopeProblem *p, uint32_t n, hipStream_t str
 // 197 / 134.  4 jobs x 500 rows, 2048 -> 2048: 48.5, alone 4.6 + 22.2 + 23.4.
 static bool share_tiled(const BlockProblem *input, uint32_t n_input, const WeightGradProblem *weight, uint32_t n_weight, bool sums)
 {
-    const Tiling &x = kInputLarge[0];
-    uint64_t tiles = 0, work = 0, longest = 0;
-    auto add = [&](uint64_t count, uint32_t depth, uint64_t slab, uint64_t rest) {
-        const uint64_t ns = std::max((depth + kSlab - 1) / kSlab, kMinSlabs) * slab + rest;
-        tiles += count;
-        work += count * ns;
-        longest = std::max(longest, ns);
-    };
-    for (uint32_t i = 0; i < n_input; ++i) add((uint64_t)((input[i].M + 127) / 128) * ((input[i].N + 127) / 128), input[i].K, x.slab, x.rest);
-    for (uint32_t i = 0; i < n_weight; ++i) add((uint64_t)((weight[i].K + 127) / 128) * ((weight[i].N + 127) / 128), weight[i].M, kWeight128.slab, kWeight128.rest);
+    const SharedTiles s = shared_tiles(input, n_input, weight, n_weight);
+    uint64_t longest = s.longest;
     const uint64_t cus = resident_grid();
-    if (tiles <= cus) longest = longest * 6 / 10;
-    const uint64_t shared = 2000 + std::max(longest, work / (2 * cus) + longest / 4);
+    if (s.tiles <= cus) longest = longest * 6 / 10;
+    const uint64_t shared = 2000 + std::max(longest, s.work / (2 * cus) + longest / 4);
     const uint64_t alone = std::min(choose(kInputLarge, input, n_input, true).ns, choose(kInputOther, input, n_input, true).ns) +
                            std::min(tiled_ns(weight, n_weight, kWeight128), tiled_ns(weight, n_weight, kWeight256));
     return shared - shared / 16 < alone + 1200 + (sums ? 3500 : 0);
@@ -414,9 +423,24 @@ hipError_t launch_gradients(const BlockProblem *input, uint32_t n_input, const W
             a.weights = (uint32_t)out;
             hipLaunchKernelGGL(gradients_few_rows, dim3(a.sums + a.inputs + a.weights), dim3(256), 0, stream, a);
         } else {
-            // all of them have a place, or places go by the work; a multiple of 8 for the XCDs
-            const uint64_t x = launch_ns(kInputLarge[0], input, n_input), y = tiled_ns(weight, n_weight, kWeight128);
-            a.inputs = (uint32_t)(in + out <= places ? in : std::min(in, std::min(places - 8, std::max<uint64_t>(8, places * x / (x + y) / 8 * 8))));
+            // All of them have a place, or places (a multiple of 8 for the XCDs) go by the work, unless whole tiles fall much better otherwise: by the time of the kind whose workgroups take longer and a
+            // quarter of the other's, a fifth less.  4 jobs x 500 rows, 2048 -> 2048, 256 and 1024 tiles, on 256 and 256 places 43.9 us, on 232 and 280 48.6; 10 x 400, 768 -> 768, 240 and 360 tiles, 21 / 23.4.
+            // Where the formula says less it is wrong as often as right: 9 jobs x 204 - 249 rows, 3280 -> 400, 14 % by the formula, 26.5 / 25.0; 13 jobs x 490, 12 %, 793 / 845.
+            uint64_t most = in;
+            if (in + out > places) {
+                const uint64_t x = shared_tiles(input, n_input, nullptr, 0).work / in, y = shared_tiles(nullptr, 0, weight, n_weight).work / out;      // of a tile, two on a compute unit
+                auto ns = [&](uint64_t i) {
+                    const uint64_t i_ns = (in + i - 1) / i * x, w_ns = (out + places - i - 1) / (places - i) * y;
+                    return std::max(i_ns, w_ns) + std::min(i_ns, w_ns) / 4;
+                };
+                const uint64_t all_x = launch_ns(kInputLarge[0], input, n_input), all_y = tiled_ns(weight, n_weight, kWeight128);
+                const uint64_t by_work = std::min(places - 8, std::max<uint64_t>(8, places * all_x / (all_x + all_y) / 8 * 8));
+                uint64_t whole = by_work;
+                for (uint64_t i = 8; i < places; i += 8)
+                    if (ns(i) < ns(whole)) whole = i;
+                most = ns(whole) * 5 < ns(by_work) * 4 ? whole : by_work;
+            }
+            a.inputs = (uint32_t)std::min(in, most);
             a.weights = (uint32_t)std::min(out, places - a.inputs);
             hipLaunchKernelGGL(gradients_tiled, dim3(a.sums + a.inputs + a.weights), dim3(256), 0, stream, a);
         }
