@@ -7,13 +7,14 @@
 
 namespace salus {
 
-// 64-row tiles, operands through an LDS ring (TileStream), two workgroups per compute unit.  Right for every size: rows and columns outside
+// 64-row tiles, operands through an LDS ring (TileStream), PER_CU workgroups per compute unit.  Right for every size: rows and columns outside
 // are neither fetched nor stored.
-template <int BM, int BN, int WM, int WN, int D, Epilogue E>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN / 2) void block_stream(BlockArgs a)
+template <int BM, int BN, int WM, int WN, int D, int PER_CU, Epilogue E>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void block_stream(BlockArgs a)
 {
     using Walk = BlockWalk<BM, BN, E>;
     using T = TileStream<BM, BN, WM, WN, !Walk::kTransposed, D, false, E == Epilogue::kGated>;
+    static_assert(PER_CU * T::kLds <= 160 * 1024, "LDS of a compute unit");
     __shared__ __attribute__((aligned(1024))) unsigned char smem[T::kLds];
     const Walk walk(a);
     T::run(walk, smem);
@@ -110,10 +111,10 @@ inline Choice choose(const Tiling (&tilings)[N], const BlockProblem *p, uint32_t
     return best;
 }
 
-template <int BM, int BN, int WM, int WN, int D, Epilogue E>
+template <int BM, int BN, int WM, int WN, int D, int PER_CU, Epilogue E>
 inline hipError_t ring(const Round &r)
 {
-    return launch_block<BlockArgs>(block_stream<BM, BN, WM, WN, D, E>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, 2 * resident_grid(), r.p, r.n, r.stream, r.launches);
+    return launch_block<BlockArgs>(block_stream<BM, BN, WM, WN, D, PER_CU, E>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, PER_CU * resident_grid(), r.p, r.n, r.stream, r.launches);
 }
 template <int BM, int BN, int WM, int WN, int PER_CU, Epilogue E, bool ONCE = false>
 inline hipError_t tiled(const Round &r)

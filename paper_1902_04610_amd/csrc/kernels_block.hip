@@ -155,6 +155,7 @@ static hipError_t narrow_grad(const Round &r)
 // average and 28, 33 and 34 % at most; the best single kind is 38 (64 x 64), 32 (64 x 128) and 25 % (32 x 32) off.  What each is for: narrow tiles fill the chip with few rows, the
 // ring streams weights past one or two row tiles, large tiles multiply.  1 job x 1 row, 4096 -> 1024: 16 columns 9.4 us, the ring 16; 32 jobs x 1 - 32 rows, 1000 -> 5520, 64 x 64 / 128 x 128 / 128 x 256
 // 75 / 73 / 73, 2760 -> 1000 37 / 37 / 55; 8 jobs x 64 rows, 2736 -> 1024, 32 x 64 / 64 x 64 20.7 / 25.8; 8 jobs x 1000 rows, 2048 -> 8192, 64 x 128 / 128 x 128 / 128 x 256 / 256 x 256 545 / 353 / 295 / 286.
+// The 64 x 64 ring: three workgroups of three stages on a compute unit, 0.99 of two of four over 27 drawn launches (0.90 - 1.0 above 512 tiles; fitted with two, and taken as 0.99 of that).
 // One 128 x 128 tile per compute unit: eight wavefronts instead of four, 4 jobs x 500 rows, 2048 -> 2048, 27.5 / 29.2 us, 2 x 2000, 1024 -> 1024, 18.3 / 19.7, 0.95 over 10 drawn launches of 130 - 256
 // tiles (gated and gate gradients: 0.98 - 1.04, not there); its time is set as the same share of the other's.
 constexpr Tiling kDense[] = {
@@ -164,7 +165,7 @@ constexpr Tiling kDense[] = {
     {32, 32, 1, 16, kAnyRows, 1100, 178, 2140, narrow<2, 2, false, Epilogue::kDense>},
     {16, 64, 2, 0, 16, 1400, 243, 3080, narrow<1, 4, true, Epilogue::kDense>},
     {32, 64, 2, 16, kAnyRows, 1800, 378, 3280, narrow<2, 4, true, Epilogue::kDense>},
-    {64, 64, 2, 0, kAnyRows, 2400, 471, 2510, ring<64, 64, 2, 2, 4, Epilogue::kDense>},
+    {64, 64, 2, 0, kAnyRows, 2400, 466, 2490, ring<64, 64, 2, 2, 3, 3, Epilogue::kDense>},
     {128, 128, 2, 0, kAnyRows, 2900, 923, 6250, tiled<128, 128, 2, 2, 2, Epilogue::kDense>},
     {128, 128, 1, 0, kAnyRows, 2800, 532, 3600, tiled<128, 128, 2, 4, 1, Epilogue::kDense>},
     {128, 256, 2, 0, kAnyRows, 2900, 1439, 10780, tiled<128, 256, 1, 4, 2, Epilogue::kDense>},
@@ -176,7 +177,7 @@ constexpr Tiling kGated[] = {      // half of a tile's columns are the gate's
     {32, 16, 1, 16, kAnyRows, 1700, 248, 1110, narrow<2, 2, false, Epilogue::kGated>},
     {16, 32, 2, 0, 16, 1400, 341, 2450, narrow<1, 4, true, Epilogue::kGated>},
     {32, 32, 2, 16, kAnyRows, 2300, 499, 1040, narrow<2, 4, true, Epilogue::kGated>},
-    {64, 64, 2, 0, kAnyRows, 2400, 806, 2280, ring<64, 128, 2, 2, 3, Epilogue::kGated>},
+    {64, 64, 2, 0, kAnyRows, 2400, 806, 2280, ring<64, 128, 2, 2, 3, 2, Epilogue::kGated>},
     {128, 64, 2, 0, kAnyRows, 2400, 1036, 3920, tiled<128, 128, 2, 2, 2, Epilogue::kGated>},
     {128, 128, 2, 0, kAnyRows, 1400, 1471, 8870, tiled<128, 256, 1, 4, 2, Epilogue::kGated>},
     {128, 128, 2, 0, 128, 1400, 1370, 8300, tiled<128, 256, 1, 4, 2, Epilogue::kGated, true>, true},
@@ -187,8 +188,8 @@ constexpr Tiling kGateGrad[] = {
     {32, 32, 1, 16, kAnyRows, 2500, 165, 830, narrow_grad<2, 2>},
     {16, 64, 1, 0, 16, 3000, 209, 270, narrow_grad<1, 4>},
     {32, 64, 1, 16, kAnyRows, 2700, 269, 1120, narrow_grad<2, 4>},
-    {64, 64, 2, 0, kAnyRows, 2000, 442, 4720, ring<64, 64, 2, 2, 4, Epilogue::kGateGrad>},
-    {64, 128, 2, 0, kAnyRows, 800, 627, 8500, ring<64, 128, 2, 2, 3, Epilogue::kGateGrad>},
+    {64, 64, 2, 0, kAnyRows, 2000, 442, 4720, ring<64, 64, 2, 2, 3, 3, Epilogue::kGateGrad>},
+    {64, 128, 2, 0, kAnyRows, 800, 627, 8500, ring<64, 128, 2, 2, 3, 2, Epilogue::kGateGrad>},
     {128, 128, 2, 0, kAnyRows, 0, 904, 14890, tiled<128, 128, 2, 2, 2, Epilogue::kGateGrad>},
     {256, 256, 1, 0, kAnyRows, 0, 1074, 19050, tiled<256, 256, 2, 4, 1, Epilogue::kGateGrad>},
 };

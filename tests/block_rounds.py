@@ -40,7 +40,7 @@ ROUNDS = [
     ("gated", jobs(4, 100, 8, 72, 1032), 0, [
         "block_narrow<2, 2, false, true, BlockFewArgs>", "block_narrow<2, 4, true, false, BlockFewArgs>"]),
     ("gated", jobs(16, 200, 72, 520, 64), 0, [
-        "block_stream<64, 128, 2, 2, 3, E1>", "block_narrow<2, 2, false, false, BlockArgs>"]),
+        "block_stream<64, 128, 2, 2, 3, 2, E1>", "block_narrow<2, 2, false, false, BlockArgs>"]),
     ("gated", jobs(16, 256, 64, 1032, 72), 0, [
         "block_tiled<256, 256, 2, 4, E1, false>", "block_narrow<2, 4, true, false, BlockArgs>"]),
     ("gated", jobs(60, 200, 1032, 72, 1000), 0, [
@@ -64,9 +64,9 @@ ROUNDS = [
     ("dense", jobs(4, 64, 520, 1032), 0, [
         "block_narrow<2, 4, true, false, BlockFewArgs>"]),
     ("dense", jobs(2, 128, 264, 4096), 0, [
-        "block_stream<64, 64, 2, 2, 4, E0>"]),
+        "block_stream<64, 64, 2, 2, 3, 3, E0>"]),
     ("dense", jobs(40, 64, 520, 520), 0, [
-        "block_stream<64, 64, 2, 2, 4, E0>"]),
+        "block_stream<64, 64, 2, 2, 3, 3, E0>"]),
     ("dense", jobs(2, 1000, 264, 4096), 0, [
         "block_tiled<128, 256, 1, 4, E0, false>"]),
     ("dense", jobs(4, 128, 64, 32768), PAST, [
@@ -86,7 +86,7 @@ ROUNDS = [
     ("gated_train", jobs(40, 16, 8, 264, 1000), 0, [
         "block_narrow<1, 4, true, true, BlockArgs>", "block_narrow<1, 4, true, false, BlockArgs>", "block_gate_grad_narrow<1, 4, BlockArgs>", "grouped_dense_bf16_narrow<1, true, 2, 8, true>", "weight_grad_few_rows", "weight_grad_few_rows"]),
     ("gated_train", jobs(4, 16, 8, 8192, 64), 0, [
-        "block_stream<64, 128, 2, 2, 3, E1>", "block_narrow<1, 1, false, false, BlockFewArgs>", "block_gate_grad_narrow<1, 4, BlockFewArgs>", "grouped_dense_bf16_narrow<1, true, 2, 8, true>", "weight_grad_few_rows"]),
+        "block_stream<64, 128, 2, 2, 3, 2, E1>", "block_narrow<1, 1, false, false, BlockFewArgs>", "block_gate_grad_narrow<1, 4, BlockFewArgs>", "grouped_dense_bf16_narrow<1, true, 2, 8, true>", "weight_grad_few_rows"]),
     ("gated_train", jobs(16, 48, 128, 8, 8), 0, [
         "block_narrow<2, 2, false, true, BlockArgs>", "block_narrow<2, 1, false, false, BlockArgs>", "block_gate_grad_narrow<2, 2, BlockArgs>", "gradients_few_rows"]),
     ("gated_train", jobs(1, 64, 8, 72, 64), 0, [
@@ -96,9 +96,9 @@ ROUNDS = [
     ("gated_train", jobs(2, 200, 64, 1000, 520), 0, [
         "block_narrow<2, 4, true, true, BlockFewArgs>", "block_narrow<2, 2, false, false, BlockFewArgs>", "block_gate_grad_narrow<2, 4, BlockFewArgs>", "grouped_dense_bf16_narrow<2, true, 2, 8, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
     ("gated_train", jobs(4, 128, 8, 1032, 8), 0, [
-        "block_stream<64, 128, 2, 2, 3, E1>", "block_narrow<2, 1, false, false, BlockFewArgs>", "block_stream<64, 64, 2, 2, 4, E2>", "grouped_dense_bf16_narrow<2, true, 2, 8, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
+        "block_stream<64, 128, 2, 2, 3, 2, E1>", "block_narrow<2, 1, false, false, BlockFewArgs>", "block_stream<64, 64, 2, 2, 3, 3, E2>", "grouped_dense_bf16_narrow<2, true, 2, 8, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
     ("gated_train", jobs(8, 500, 8, 264, 8), 0, [
-        "block_tiled<128, 128, 2, 2, E1, false>", "block_narrow<2, 1, false, false, BlockArgs>", "block_stream<64, 128, 2, 2, 3, E2>", "gradients_tiled"]),
+        "block_tiled<128, 128, 2, 2, E1, false>", "block_narrow<2, 1, false, false, BlockArgs>", "block_stream<64, 128, 2, 2, 3, 2, E2>", "gradients_tiled"]),
     ("gated_train", jobs(60, 100, 8, 2048, 128), 0, [
         "block_tiled<128, 256, 1, 4, E1, false>", "block_tiled<128, 256, 1, 4, E1, false>", "block_narrow<2, 4, true, false, BlockArgs>", "block_narrow<2, 4, true, false, BlockArgs>", "block_tiled<128, 128, 2, 2, E2, false>", "block_tiled<128, 128, 2, 2, E2, false>", "grouped_dense_bf16_narrow<2, true, 2, 8, false>", "weight_grad_few_rows", "weight_grad_few_rows"]),
     ("gated_train", jobs(1, 2048, 8, 8192, 8), 0, [
@@ -114,11 +114,11 @@ ROUNDS = [
     ("dense_train", jobs(40, 5, 8, 64), 0, [
         "block_narrow<1, 1, false, false, BlockArgs>", "block_slope", "grouped_dense_bf16_narrow<1, true, 2, 8, true>", "weight_grad_few_rows"]),
     ("dense_train", jobs(40, 200, 264, 72), 0, [
-        "block_stream<64, 64, 2, 2, 4, E0>", "block_slope", "block_column_sums", "block_column_sums", "block_tiled<128, 128, 2, 2, E3, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
+        "block_stream<64, 64, 2, 2, 3, 3, E0>", "block_slope", "block_column_sums", "block_column_sums", "block_tiled<128, 128, 2, 2, E3, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
     ("dense_train", jobs(1, 256, 8, 8), 0, [
         "block_narrow<2, 1, false, false, BlockFewArgs>", "block_slope", "gradients_tiled"]),
     ("dense_train", jobs(60, 500, 8, 8), 0, [
-        "block_stream<64, 64, 2, 2, 4, E0>", "block_stream<64, 64, 2, 2, 4, E0>", "block_slope", "block_slope", "block_column_sums", "block_column_sums", "grouped_dense_bf16_stream<64, 128, 2, 2, 1, true, 3>", "weight_grad_tiled<128, 128, 2, 2>"]),
+        "block_stream<64, 64, 2, 2, 3, 3, E0>", "block_stream<64, 64, 2, 2, 3, 3, E0>", "block_slope", "block_slope", "block_column_sums", "block_column_sums", "grouped_dense_bf16_stream<64, 128, 2, 2, 1, true, 3>", "weight_grad_tiled<128, 128, 2, 2>"]),
     ("dense_train", jobs(60, 48, 128, 8), 0, [
         "block_narrow<2, 1, false, false, BlockArgs>", "block_narrow<2, 1, false, false, BlockArgs>", "block_slope", "block_slope", "block_column_sums", "block_column_sums", "grouped_dense_bf16_narrow<2, true, 2, 8, true>", "grouped_dense_bf16_stream<64, 64, 2, 1, 2, true, 4>", "weight_grad_few_rows"]),
     ("dense_train", jobs(8, 97, 264, 520), 0, [
@@ -130,9 +130,9 @@ ROUNDS = [
     ("dense_train", jobs(1, 24, 1032, 4096), 0, [
         "block_narrow<2, 1, false, false, BlockFewArgs>", "block_slope", "gradients_few_rows"]),
     ("dense_train", jobs(4, 300, 520, 520), 0, [
-        "block_stream<64, 64, 2, 2, 4, E0>", "block_slope", "gradients_tiled"]),
+        "block_stream<64, 64, 2, 2, 3, 3, E0>", "block_slope", "gradients_tiled"]),
     ("dense_train", jobs(1, 150, 4096, 4096), 0, [
-        "block_stream<64, 64, 2, 2, 4, E0>", "block_slope", "block_column_sums", "grouped_dense_bf16_stream<64, 64, 2, 1, 2, true, 4>", "weight_grad_tiled<256, 256, 2, 4>"]),
+        "block_stream<64, 64, 2, 2, 3, 3, E0>", "block_slope", "block_column_sums", "grouped_dense_bf16_stream<64, 64, 2, 1, 2, true, 4>", "weight_grad_tiled<256, 256, 2, 4>"]),
     ("dense_train", jobs(1, 4001, 4088, 520), 0, [
         "block_tiled<128, 128, 2, 4, E0, false>", "block_slope", "block_column_sums", "block_tiled<256, 256, 2, 4, E3, false>", "weight_grad_tiled<128, 128, 2, 2>"]),
     ("clip", [(100, 9)] * 3, 0, [
