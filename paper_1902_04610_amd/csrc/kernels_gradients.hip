@@ -376,7 +376,7 @@ static SharedTiles shared_tiles(const BlockProblem *input, uint32_t n_input, con
 // the longest for the end, of which a sixteenth is taken off: they measured that much quicker than this says; against the quickest launches of their own and 1.2 us for each that is saved (a launch
 // that adds columns: 3.5).  Training calls of drawn sizes: 0.90 of the time where this shares; over 43 of them 0.97 if
 // always shared, with 0.66 - 1.47 at the ends: 5 jobs x 125 - 262 rows, 704 -> 112, 18.9 / 28.4 us, 1 job x 486 rows, depth 14224, whose few input gradient tiles one compute unit walks alone,
-// 197 / 134.  4 jobs x 500 rows, 2048 -> 2048: 48.5, alone 4.6 + 22.2 + 23.4.
+// 197 / 134.  4 jobs x 500 rows, 2048 -> 2048: 43.9, alone 4.6 + 22.2 + 23.4.
 static bool share_tiled(const BlockProblem *input, uint32_t n_input, const WeightGradProblem *weight, uint32_t n_weight, bool sums)
 {
     const SharedTiles s = shared_tiles(input, n_input, weight, n_weight);
