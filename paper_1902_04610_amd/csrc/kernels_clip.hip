@@ -64,26 +64,18 @@ __device__ inline double block_sum_f64(double v)
 
 __device__ inline double square(float v) { return (double)v * (double)v; }
 
-// The squares of 16 bytes.  Those of bf16 numbers are exact in float, and eight of them are added there if that can neither overflow nor lose all of them.
+// The squares of 16 bytes, in 64 bits whatever the type: eight squares of bf16 numbers added in float would lose all that are below 2^-24 of the first.
 template <bool BF16>
 __device__ inline double squares(u32x4 w)
 {
     if constexpr (BF16) {
-        float v[8], most = 0.0f;
+        double low = 0, high = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            v[2 * i] = bf16_low(w[i]);
-            v[2 * i + 1] = bf16_high(w[i]);
-            most = fmaxf(most, fmaxf(fabsf(v[2 * i]), fabsf(v[2 * i + 1])));
+            low += square(bf16_low(w[i]));
+            high += square(bf16_high(w[i]));
         }
-        float q = v[0] * v[0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) q = fmaf(v[i], v[i], q);
-        if (most > 0x1p-50f && most < 0x1p50f) return (double)q;      // also with a NaN beside ordinary numbers: q is one then
-        double s = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += square(v[i]);
-        return s;
+        return low + high;
     } else {
         return (square(as_float(w[0])) + square(as_float(w[1]))) + (square(as_float(w[2])) + square(as_float(w[3])));
     }
