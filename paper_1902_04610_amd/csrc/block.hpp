@@ -37,13 +37,12 @@ enum class Epilogue { kDense, kGated, kGateGrad, kPlainT };
 
 // ---- activations ------------------------------------------------------------------------------------------------------------
 // NaNs pass through all of them, as they do through the products.
-// Upper tail of the normal distribution at x >= 0: 2^p(x), p the polynomial of degree 8 that minimizes the largest x |2^p - Q| over [0, 6] (1e-8; fitted
-// by linear programming).  With it GELU(z) = z / 2 + |z| (1/2 - Q) is off by less than 8e-8 of |z| in float arithmetic (the library's erfc takes four
-// times as long: 24 jobs x 1 - 128 rows, 1000 -> 3080, float results, 9 of 49 us) and Phi by 1.3e-7, which is enough for results
-// that stay floats.  gelu_fast, two degrees less, suffices where a bf16 is next.
-__device__ inline float normal_tail(float x)
+// Upper tail of the normal distribution at c in [0, 9]: 2^p(c), p the polynomial of degree 8 that minimizes the largest c |2^p - Q| over [0, 6] (1e-8; fitted
+// by linear programming), so Phi is off by 1.3e-7.  GELU(z) is z Q for negative z and z - z Q for others: max(z, 0) - |z| Q, which subtracts nothing from a negative z's
+// small result.  (The library's erfc takes four times as long: 24 jobs x 1 - 128 rows, 1000 -> 3080, float results, 9 of 49 us.)  gelu_fast, two degrees less,
+// suffices where a bf16 is next.
+__device__ inline float tail_exponent(float c)
 {
-    const float c = fminf(x, 9.0f);
     float p = fmaf(-1.8847762248697109e-06f, c, 2.7810900064650923e-05f);
     p = fmaf(p, c, -0.00013004051288589835f);
     p = fmaf(p, c, -0.0002765035897027701f);
@@ -51,8 +50,22 @@ __device__ inline float normal_tail(float x)
     p = fmaf(p, c, -0.0526358038187027f);
     p = fmaf(p, c, -0.4591573178768158f);
     p = fmaf(p, c, -1.15111243724823f);
-    p = fmaf(p, c, -0.9999998211860657f);
-    return __builtin_amdgcn_exp2f(p);
+    return fmaf(p, c, -0.9999998211860657f);
+}
+__device__ inline float normal_tail(float c) { return __builtin_amdgcn_exp2f(tail_exponent(c)); }
+// The same at c in [0, 13] for results that stay floats: from 3.25 on, where an absolute error of Q is no small part of it any more, the polynomial of degree 7 that minimizes
+// the largest |p - log2 Q| over [3.25, 13].  GELU of it is off by less than 1.2e-7 of |z|, and for negative z by less than 2.1e-5 of itself down to -12.9, where it is 3e-37
+// (in float arithmetic).
+__device__ inline float normal_tail_far(float c)
+{
+    float p = fmaf(-6.624220816320303e-08f, c, 4.464800895220833e-06f);
+    p = fmaf(p, c, -0.00013070812565274537f);
+    p = fmaf(p, c, 0.0021917573176324368f);
+    p = fmaf(p, c, -0.02350013330578804f);
+    p = fmaf(p, c, -0.5481355786323547f);
+    p = fmaf(p, c, -1.0025348663330078f);
+    p = fmaf(p, c, -1.106598138809204f);
+    return __builtin_amdgcn_exp2f(c < 3.25f ? tail_exponent(c) : p);
 }
 // exp's argument is off by 2^-24 of itself, which the slope of the sigmoid takes back: 3e-8 of |z| at most in z sigmoid(z), beside the last bits of v_exp_f32 and v_rcp_f32.
 __device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
@@ -67,7 +80,10 @@ __device__ inline void activate_all(float (&z)[N], uint32_t act, bool fine)
         for (int i = 0; i < N; ++i) z[i] = relu_nan(z[i]);
     } else if (act == 2 && fine) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = fmaf(fabsf(z[i]), 0.5f - normal_tail(fabsf(z[i])), 0.5f * z[i]);
+        for (int i = 0; i < N; ++i) {
+            const float c = fminf(fabsf(z[i]), 13.0f);      // beyond it, also at an infinity, nothing is left of a negative z
+            z[i] = fmaf(-c, normal_tail_far(c), relu_nan(z[i]));
+        }
     } else if (act == 2) {
 #pragma unroll
         for (int i = 0; i < N; ++i) z[i] = gelu_fast(z[i]);
@@ -90,9 +106,9 @@ __device__ inline void activate_with_slope(const float (&z)[N], float (&a)[N], f
     } else if (act == 2) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float x = fabsf(z[i]), q = normal_tail(x);
+            const float c = fminf(fabsf(z[i]), 9.0f), q = normal_tail(c);
             const float phi = 0.39894228040143267794f * __builtin_amdgcn_exp2f(-0.72134752f * z[i] * z[i]);
-            a[i] = fmaf(x, 0.5f - q, 0.5f * z[i]);
+            a[i] = fmaf(-c, q, relu_nan(z[i]));
             d[i] = fmaf(z[i], phi, z[i] < 0.0f ? q : 1.0f - q);
         }
     } else if (act == 3) {
