@@ -33,7 +33,7 @@ def act(z, kind):
 
 def slope(z, kind):
     if kind == RELU:
-        return (z > 0).astype(np.float64)
+        return np.where(np.isnan(z), z, (z > 0).astype(np.float64))
     if kind == GELU:
         return 0.5 * erfc(-z / np.sqrt(2)) + z * np.exp(-z * z / 2) / np.sqrt(2 * np.pi)
     if kind == SILU:
