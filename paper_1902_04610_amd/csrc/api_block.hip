@@ -113,10 +113,11 @@ int32_t gated_forward(salus_pool_t *pool, const salus_gated_desc *descs, uint32_
         if (d.gu_off != SALUS_ABSENT) lane.write(d.gu_off, M * d.F * 8);
         if (lane.outside()) return kLane;
         if (lane.overlap()) return kOverlap;
+        const uint32_t flags = kOutBf16 | (d.gu_off != SALUS_ABSENT ? kReadAgain : 0u);
         in.push_back({at.persist + d.w_in_off, at.lane + d.x_off, at.lane + d.h_off, nullptr, (float *)at_or_null(at.lane, d.gu_off), nullptr,
-                      d.M, d.K, d.F, (uint32_t)d.act | kOutBf16});
+                      d.M, d.K, d.F, (uint32_t)d.act | flags});
         out.push_back({at.persist + d.w_out_off, at.lane + d.h_off, at.lane + d.y_off, at_or_null(at.lane, d.r_off), nullptr, nullptr, d.M, d.F, d.N,
-                       (uint32_t)SALUS_ACT_NONE | kOutBf16});
+                       (uint32_t)SALUS_ACT_NONE | flags});
         return nullptr;
     });
     if (rc) return rc;
@@ -188,7 +189,7 @@ int32_t dense_forward(salus_pool_t *pool, const salus_dense_desc *descs, uint32_
         if (lane.outside()) return kLane;
         if (lane.overlap()) return kOverlap;
         problems.push_back({at.persist + d.w_off, at.lane + d.x_off, at.lane + d.y_off, at_or_null(at.lane, d.r_off), (float *)at_or_null(at.lane, d.z_off),
-                            at_or_null(at.persist, d.b_off), d.M, d.K, d.N, (uint32_t)d.act | (d.y_dtype == SALUS_BF16 ? kOutBf16 : 0u)});
+                            at_or_null(at.persist, d.b_off), d.M, d.K, d.N, (uint32_t)d.act | (d.y_dtype == SALUS_BF16 ? kOutBf16 : 0u) | (d.z_off != SALUS_ABSENT ? kReadAgain : 0u)});
         return nullptr;
     });
     if (rc) return rc;

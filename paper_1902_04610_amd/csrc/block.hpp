@@ -15,8 +15,9 @@ struct BlockProblem {
     float *Z;            // dense, gated: M x N (M x 2 N) floats in front of the activation, written if not null; gate gradient: read
     const void *B;       // dense: N bf16 added in front of the activation, or null
     uint32_t M, K, N;
-    uint32_t flags;      // bits 0-7 activation; kOutBf16
+    uint32_t flags;      // bits 0-7 activation; kOutBf16, kReadAgain
 };
+constexpr uint32_t kReadAgain = 1u << 16;    // for the launcher: a backward pass will read W again
 constexpr uint32_t kBlockProblems = 56;      // of a launch
 struct BlockArgs {
     uint32_t n, tiles, pad[2];

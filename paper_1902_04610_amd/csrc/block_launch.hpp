@@ -95,15 +95,15 @@ inline Choice choose(const Tiling (&tilings)[N], const BlockProblem *p, uint32_t
 {
     uint32_t rows = 0;
     uint64_t bytes = 0;
-    bool kept = false;       // for a backward pass, which reads the weights again
+    bool again = false;      // a backward pass, as what the forward pass leaves for it tells
     for (uint32_t i = 0; i < n; ++i) {
         rows = std::max(rows, p[i].M);
         bytes += (uint64_t)column_bytes * p[i].K * p[i].N;
-        kept = kept || p[i].Z;
+        again = again || (p[i].flags & kReadAgain);
     }
     Choice best{nullptr, ~0ull};
     for (const Tiling &t : tilings) {
-        if (rows <= t.above || rows > t.upto || (t.once && (cached || kept))) continue;
+        if (rows <= t.above || rows > t.upto || (t.once && (cached || again))) continue;
         uint64_t ns = launch_ns(t, p, n);
         if (!cached) ns = std::max(ns, bytes / (t.once ? kStreamOnce : t.bm < 64 ? kStreamNarrow : kStream));
         if (ns < best.ns) best = {&t, ns};
