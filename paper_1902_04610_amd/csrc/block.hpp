@@ -20,7 +20,7 @@ struct BlockProblem {
 constexpr uint32_t kReadAgain = 1u << 16;    // for the launcher: a backward pass will read W again
 constexpr uint32_t kBlockProblems = 56;      // of a launch
 struct BlockArgs {
-    uint32_t n, tiles, pad[2];
+    uint32_t n, tiles, base, pad;            // base: kernels of one tile per workgroup begin with this one
     uint32_t first[kBlockProblems];          // first tile of problem i; kNoTile from n on
     BlockProblem p[kBlockProblems];
 };
@@ -28,10 +28,25 @@ static_assert(sizeof(BlockArgs) <= 4096, "kernel arguments are limited to 4 KB")
 // The same for launches of few problems, whose time is the host's.
 constexpr uint32_t kBlockFew = 4;
 struct BlockFewArgs {
-    uint32_t n, tiles, pad[2];
+    uint32_t n, tiles, base, pad;
     uint32_t first[kBlockFew];
     BlockProblem p[kBlockFew];
 };
+
+// A grid has fewer than 2^32 threads: kernels of one tile per workgroup, which have 256, take more tiles in several launches (of a multiple of 8, for the XCDs).
+// launch(workgroups, first tile).
+constexpr uint64_t kMostBlocks = 1u << 23;
+template <typename Launch>
+inline hipError_t launch_tiles(uint64_t tiles, uint64_t *launches, Launch launch)
+{
+    for (uint64_t base = 0; base < tiles; base += kMostBlocks) {
+        launch((uint32_t)(tiles - base < kMostBlocks ? tiles - base : kMostBlocks), (uint32_t)base);
+        if (launches) *launches += 1;
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 // What a product's sums become: Y = act(X W + B) + R; Y = act(X Wg) * (X Wu); [dG dU] of dH = X W^T; X W^T itself.
 enum class Epilogue { kDense, kGated, kGateGrad, kPlainT };

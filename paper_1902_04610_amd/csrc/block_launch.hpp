@@ -44,11 +44,11 @@ inline hipError_t launch_block(void (*kernel)(Args), int threads, uint32_t bm, u
         Args a{};
         const uint64_t tiles = fill_group(a, p + at, std::min(kMost, n - at),
                                           [&](const BlockProblem &q) { return (uint64_t)((q.M + bm - 1) / bm) * ((q.N + cols - 1) / cols); });
-        if (tiles == 0) continue;
         if (tiles > 0x7fffffffull) return hipErrorInvalidValue;
-        hipLaunchKernelGGL(kernel, dim3(grid ? (uint32_t)std::min<uint64_t>(tiles, grid) : (uint32_t)tiles), dim3(threads), 0, stream, a);
-        if (launches) *launches += 1;
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch_tiles(grid ? std::min<uint64_t>(tiles, grid) : tiles, launches, [&](uint32_t blocks, uint32_t base) {
+            a.base = base;
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, stream, a);
+        });
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -17,7 +17,7 @@ __device__ inline void narrow_block(const Args &a, unsigned char *smem)
     using T = std::conditional_t<TWO, NarrowTile<MT, NB, 1, 80 * 1024>, NarrowTile<MT, NB>>;
     constexpr uint32_t kCols = GATED ? 8 * NB : 16 * NB;
     BlockProblem p;
-    const uint32_t t = find_owner(a.first, a.p, xcd_remap(blockIdx.x, a.tiles), p);
+    const uint32_t t = find_owner(a.first, a.p, xcd_remap(blockIdx.x + a.base, a.tiles), p);
     const uint32_t M = p.M, N = p.N, act = p.flags & 0xffu, rt = (M + 16 * MT - 1) / (16 * MT);
     const Tile tile = {t % rt * 16 * MT, t / rt * kCols};      // row tiles of one column tile are neighbours: they share W
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kGemmThreads) void block_gate_grad_narrow(Args a)
 {
     __shared__ float lds[reduce_lds_floats<MT * CPL>()];
     BlockProblem p;
-    const uint32_t t = find_owner(a.first, a.p, xcd_remap(blockIdx.x, a.tiles), p), rt = (p.M + 16 * MT - 1) / (16 * MT);
+    const uint32_t t = find_owner(a.first, a.p, xcd_remap(blockIdx.x + a.base, a.tiles), p), rt = (p.M + 16 * MT - 1) / (16 * MT);
     const Tile tile = {t % rt * 16 * MT, t / rt * 16 * CPL};
     if (p.K > kGateDeepK) narrow_gate_grad<MT, CPL, 16 / CPL>(p, tile, lds);
     else narrow_gate_grad<MT, CPL, 2>(p, tile, lds);
@@ -213,7 +213,7 @@ hipError_t launch_block_gate_grad(const BlockProblem *p, uint32_t n, bool cached
 // eight columns; all of a lane's loads are on their way together.  The four wavefronts' sums are added in the order of the rows.  Bound by memory:
 // 8 bytes an element (2 and 4 read, 2 written).
 struct SlopeArgs {
-    uint32_t n, tiles, pad[2];
+    uint32_t n, tiles, base, pad;
     uint32_t first[kBlockProblems];
     SlopeProblem p[kBlockProblems];
 };
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(64 * kWaves) void block_slope(SlopeArgs a)
 {
     __shared__ float part[kWaves][8][64];
     SlopeProblem p;
-    const uint32_t t = find_owner(a.first, a.p, blockIdx.x, p), ct = (p.N + kSlopeCols - 1) / kSlopeCols;
+    const uint32_t t = find_owner(a.first, a.p, blockIdx.x + a.base, p), ct = (p.N + kSlopeCols - 1) / kSlopeCols;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t block = t / ct, row0 = block * kSlopeRows + wave * kSlopeWaveRows, c = (t % ct) * kSlopeCols + 8 * lane;
     const bool in = c < p.N;
@@ -289,11 +289,10 @@ hipError_t launch_block_slope(const SlopeProblem *p, uint32_t n, hipStream_t str
             return q.dZ || q.db ? (uint64_t)((q.M + kSlopeRows - 1) / kSlopeRows) * ((q.N + kSlopeCols - 1) / kSlopeCols) : 0;
         });
         if (tiles > 0x7fffffffull) return hipErrorInvalidValue;
-        if (tiles) {
-            hipLaunchKernelGGL(block_slope, dim3((uint32_t)tiles), dim3(256), 0, stream, a);
-            if (launches) *launches += 1;
-        }
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch_tiles(tiles, launches, [&](uint32_t blocks, uint32_t base) {
+            a.base = base;
+            hipLaunchKernelGGL(block_slope, dim3(blocks), dim3(256), 0, stream, a);
+        });
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
