@@ -348,12 +348,7 @@ class Pool:
     @staticmethod
     def _make(kind, items):
         items = list(items)
-        names = [name for name, _ in kind._fields_]
-        for it in items:
-            if not set(it) <= set(names):
-                raise ValueError(f"{kind.__name__} has no {sorted(set(it) - set(names))}")
-        return (kind * len(items))(*[kind(*[it.get(name, ABSENT) if name.endswith("_off") else it[name] for name in names])
-                                     for it in items]), []
+        return (kind * len(items))(*[_filled(kind, it) for it in items]), []
 
     @staticmethod
     def make_gated_descs(items):
@@ -381,11 +376,13 @@ class Pool:
         """dicts(job, tensors=[dict(g_off, count, dtype[, wm_off, wb_off])], max_norm[, lr], norm_off, work_off)"""
         items = list(items)
         keep = [_clip_tensors(it["tensors"]) for it in items]
-        arr = (ClipDesc * len(items))(*[ClipDesc(it["job"], len(t), t, it["max_norm"], it.get("lr", 0.0), it["norm_off"], it["work_off"])
+        arr = (ClipDesc * len(items))(*[_filled(ClipDesc, {"lr": 0.0, **it, "tensors": C.cast(t, C.POINTER(ClipTensor))}, n_tensors=len(t))
                                         for it, t in zip(items, keep)])
         return arr, keep
 
     def _grouped(self, call, descs, n, stream):
+        if n is not None and not 0 <= n <= len(descs):
+            raise ValueError(f"n is {n}, of {len(descs)} descriptors")
         return self._check(getattr(self._lib, call)(self._h, descs, len(descs) if n is None else n, stream),
                            (OK, EINVAL, ENOTRESIDENT, EBUSY))
 
@@ -457,17 +454,32 @@ def train_work_bytes(M, layers):
     return lib().salus_train_work_bytes(M, L, len(layers))
 
 
+def _fits(ctype, name, value):
+    """value, which ctypes would cut to its field without a word."""
+    if ctype in (C.c_int32, C.c_uint32, C.c_uint64) and ctype(value).value != value:
+        raise ValueError(f"{name} = {value} does not fit")
+    return value
+
+
+def _filled(kind, item, **more):
+    """A descriptor of a transformer-block call from a dict and what is not the caller's to give; an offset that is left out is ABSENT."""
+    names = [name for name, _ in kind._fields_ if name not in more and name != "pad"]
+    if not set(item) <= set(names):
+        raise ValueError(f"{kind.__name__} has no {sorted(set(item) - set(names))}")
+    given = {name: item.get(name, ABSENT) if name.endswith("_off") else item[name] for name in names}
+    return kind(**{name: _fits(ctype, name, value) for name, ctype in kind._fields_ for value in [{**given, **more}.get(name, 0)]})
+
+
 def gated_grad_work_bytes(M, F):
-    return lib().salus_gated_grad_work_bytes(M, F)
+    return lib().salus_gated_grad_work_bytes(_fits(C.c_uint32, "M", M), _fits(C.c_uint32, "F", F))
 
 
 def dense_grad_work_bytes(M, N):
-    return lib().salus_dense_grad_work_bytes(M, N)
+    return lib().salus_dense_grad_work_bytes(_fits(C.c_uint32, "M", M), _fits(C.c_uint32, "N", N))
 
 
 def _clip_tensors(tensors):
-    return (ClipTensor * len(tensors))(*[ClipTensor(t["g_off"], t["count"], t.get("wm_off", ABSENT), t.get("wb_off", ABSENT), t["dtype"])
-                                         for t in tensors])
+    return (ClipTensor * len(tensors))(*[_filled(ClipTensor, t) for t in tensors])
 
 
 def clip_work_bytes(tensors):
