@@ -50,11 +50,15 @@ private:
     std::vector<Range> r_;
 };
 
-// Nothing is thrown across the C boundary.
-template <typename F>
-int32_t guarded(F body)
+// A call's body, if there is anything to do and to do it with.  Nothing is thrown across the C boundary.
+template <typename Desc, typename F>
+int32_t guarded(salus_pool_t *pool, const Desc *descs, uint32_t n, F body)
 {
+    if (!pool) return SALUS_EINVAL;
+    if (n == 0) return SALUS_OK;
     try {
+        if (!descs) return pool_error(pool, SALUS_EINVAL, "null descriptor array");
+        if (!has_device(pool)) return pool_error(pool, SALUS_EINVAL, "pool has no device memory");
         return body();
     } catch (const std::bad_alloc &) {
         return SALUS_ENOMEM;
@@ -74,8 +78,6 @@ const char *const kOverlap = "a buffer that is written overlaps another one";
 template <typename Desc, typename Place>
 int32_t for_jobs(salus_pool_t *pool, const Desc *descs, uint32_t n, Place place)
 {
-    if (!descs) return pool_error(pool, SALUS_EINVAL, "null descriptor array");
-    if (!has_device(pool)) return pool_error(pool, SALUS_EINVAL, "pool has no device memory");
     std::vector<int32_t> lanes_used;
     lanes_used.reserve(n);
     for (uint32_t i = 0; i < n; ++i) {
@@ -283,25 +285,19 @@ extern "C" {
 
 int32_t salus_grouped_gated_forward(salus_pool_t *pool, const salus_gated_desc *descs, uint32_t n, void *stream)
 {
-    if (!pool) return SALUS_EINVAL;
-    if (n == 0) return SALUS_OK;
-    return guarded([&] { return gated_forward(pool, descs, n, (hipStream_t)stream); });
+    return guarded(pool, descs, n, [&] { return gated_forward(pool, descs, n, (hipStream_t)stream); });
 }
 
 uint64_t salus_gated_grad_work_bytes(uint32_t M, uint32_t F) { return up256((uint64_t)M * F * 4); }      // [dG dU]
 
 int32_t salus_grouped_gated_backward(salus_pool_t *pool, const salus_gated_grad_desc *descs, uint32_t n, void *stream)
 {
-    if (!pool) return SALUS_EINVAL;
-    if (n == 0) return SALUS_OK;
-    return guarded([&] { return gated_backward(pool, descs, n, (hipStream_t)stream); });
+    return guarded(pool, descs, n, [&] { return gated_backward(pool, descs, n, (hipStream_t)stream); });
 }
 
 int32_t salus_grouped_dense_forward(salus_pool_t *pool, const salus_dense_desc *descs, uint32_t n, void *stream)
 {
-    if (!pool) return SALUS_EINVAL;
-    if (n == 0) return SALUS_OK;
-    return guarded([&] { return dense_forward(pool, descs, n, (hipStream_t)stream); });
+    return guarded(pool, descs, n, [&] { return dense_forward(pool, descs, n, (hipStream_t)stream); });
 }
 
 // dZ, then the column sums of its blocks of rows
@@ -312,9 +308,7 @@ uint64_t salus_dense_grad_work_bytes(uint32_t M, uint32_t N)
 
 int32_t salus_grouped_dense_backward(salus_pool_t *pool, const salus_dense_grad_desc *descs, uint32_t n, void *stream)
 {
-    if (!pool) return SALUS_EINVAL;
-    if (n == 0) return SALUS_OK;
-    return guarded([&] { return dense_backward(pool, descs, n, (hipStream_t)stream); });
+    return guarded(pool, descs, n, [&] { return dense_backward(pool, descs, n, (hipStream_t)stream); });
 }
 
 uint64_t salus_clip_work_bytes(const salus_clip_tensor *tensors, uint32_t n_tensors)
@@ -325,16 +319,12 @@ uint64_t salus_clip_work_bytes(const salus_clip_tensor *tensors, uint32_t n_tens
 
 int32_t salus_grouped_clip(salus_pool_t *pool, const salus_clip_desc *descs, uint32_t n, void *stream)
 {
-    if (!pool) return SALUS_EINVAL;
-    if (n == 0) return SALUS_OK;
-    return guarded([&] { return clip(pool, descs, n, false, (hipStream_t)stream); });
+    return guarded(pool, descs, n, [&] { return clip(pool, descs, n, false, (hipStream_t)stream); });
 }
 
 int32_t salus_grouped_clip_sgd(salus_pool_t *pool, const salus_clip_desc *descs, uint32_t n, void *stream)
 {
-    if (!pool) return SALUS_EINVAL;
-    if (n == 0) return SALUS_OK;
-    return guarded([&] { return clip(pool, descs, n, true, (hipStream_t)stream); });
+    return guarded(pool, descs, n, [&] { return clip(pool, descs, n, true, (hipStream_t)stream); });
 }
 
 }  // extern "C"
