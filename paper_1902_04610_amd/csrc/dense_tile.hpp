@@ -9,16 +9,11 @@ namespace salus {
 // of every 16x16 block holds row 4*(lane/16)+r, so wavefront w ends up owning
 // rows with r == w: each wavefront sends the other three quarters through LDS
 // and adds what it receives in a fixed order.
-constexpr int sums_per_pass(int n)
-{
-    int g = n < 16 ? n : 16;
-    while (n % g != 0) --g;
-    return g;
-}
 template <int NACC>
 __device__ inline void reduce_scatter(f32x4 (&acc)[NACC], float (&own)[NACC], float *lds)
 {
-    constexpr int G = sums_per_pass(NACC);      // accumulators per pass (bounds the LDS footprint)
+    constexpr int G = NACC < 16 ? NACC : 16;    // accumulators per pass (bounds the LDS footprint)
+    static_assert(NACC % G == 0, "whole passes");
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // lds[dst wave][source slot][accumulator in pass][lane]
@@ -48,7 +43,7 @@ __device__ inline void reduce_scatter(f32x4 (&acc)[NACC], float (&own)[NACC], fl
 }
 
 template <int NACC>
-constexpr int reduce_lds_floats() { return kWaves * 3 * sums_per_pass(NACC) * 64; }
+constexpr int reduce_lds_floats() { return kWaves * 3 * (NACC < 16 ? NACC : 16) * 64; }
 
 // ---------------------------------------------------------------------------
 // bf16 weights and activations, float accumulation, v_mfma_f32_16x16x32_bf16.

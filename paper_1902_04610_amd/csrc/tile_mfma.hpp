@@ -411,7 +411,7 @@ struct TilePair {
     typedef f32x16 Acc[FN][FM];
 
     template <typename Walk>
-    __device__ static void run(const Walk &walk, unsigned char *smem, uint32_t begin = blockIdx.x, uint32_t stride = gridDim.x)
+    __device__ static void run(const Walk &walk, unsigned char *smem)
     {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -423,7 +423,7 @@ struct TilePair {
         fn.init(wn * (32u * FN), lane);
 
         const uint32_t tiles = walk.tiles();
-        uint32_t id = begin;                // of the tile that the M stream walks towards
+        uint32_t id = blockIdx.x;                // of the tile that the M stream walks towards
         typename Walk::Place ahead = walk.place(id), cur = ahead;
         uint32_t cur_id = id;
         SM sm;
@@ -435,7 +435,7 @@ struct TilePair {
         // Crossed into right before the first request of the next tile, the M side first (k-step 3 of the last but one slab).
         auto cross_m = [&]() {
             if (sm.slabs_left != 0) return;
-            id += stride;
+            id += gridDim.x;
             if (id < tiles) {
                 ahead = walk.place(id);
                 sm.locate(walk.m(ahead), ahead.m0, wave);
@@ -535,7 +535,7 @@ struct TilePair {
                 if (!landed) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 landed = true;
             });
-            cur_id += stride;
+            cur_id += gridDim.x;
             if (cur_id >= tiles) {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may arrive in LDS after this workgroup
                 break;
@@ -550,12 +550,12 @@ struct TilePair {
 // tiles keeps it full through the epilogues.  One barrier per slab: after it slab s has landed for everyone
 // and everyone has left the stage of slab s - 1, which is requested into at once.  HALVES: two sums per output, over the first and
 // over the second two k-steps of every slab, added at the end of a tile.
-template <int BM, int BN, int WM, int WN, bool TRN, int D, bool HALVES = false, bool PAIRS = false, bool ONCE = false>
+template <int BM, int BN, int WM, int WN, bool TRN, int D, bool HALVES = false, bool PAIRS = false>
 struct TileStream {
     static constexpr int kWavesT = WM * WN, kThreads = 64 * kWavesT;
     static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;
     using SM = OperandStream<BM, false, kWavesT, D>;
-    using SN = OperandStream<BN, TRN, kWavesT, D, kSlab, ONCE, PAIRS>;
+    using SN = OperandStream<BN, TRN, kWavesT, D, kSlab, false, PAIRS>;
     static constexpr uint32_t kLds = SM::kRing + SN::kRing;
     static constexpr int kBehind = (D - 2) * (SM::I + SN::I);
     static_assert(kLds <= 160 * 1024 && kBehind <= 63, "LDS of a compute unit, largest count of s_waitcnt");
