@@ -76,14 +76,14 @@ def gated_forward(x, w_in, w_out, r, kind):
     return dict(gu=rounded(gu, egu, False), h=(h, eh), y=rounded(y, ey))
 
 
-def gated_backward(x, w_in, w_out, h, gu, dy, kind):
-    """From what the forward pass left in h (bf16) and gu (float)."""
+def gated_backward(x, w_in, w_out, h, gu, dy, kind, fine=False):
+    """From what the forward pass left in h (bf16) and gu (float).  fine: slopes within what dense_backward allows, 8 steps of 2^-24 (1 + |z|)."""
     F = w_out.shape[0]
     g, u = gu[:, :F], gu[:, F:]
     dh, edh = product(dy, w_out.T)
     a, ea = activated(g, 0.0, kind)
     d = slope(g, kind)
-    ed = np.zeros_like(d) if kind in (NONE, RELU) else np.full_like(d, 3e-5)
+    ed = np.zeros_like(d) if kind in (NONE, RELU) else 8 * STEP * (1 + np.abs(g)) if fine else np.full_like(d, 3e-5)
     dg = dh * u * d
     edg = edh * np.abs(u * d) + np.abs(dh * u) * ed + edh * np.abs(u) * ed + 3 * STEP * np.abs(dg)
     du = dh * a
