@@ -135,7 +135,7 @@ __device__ inline void dense_bf16_sums(const P &p, const Tile tile, float *lds, 
             // column i of the 8 x CPL block: dword j = (row 2j, row 2j+1)
             u32x4 b;
             if constexpr (TW) {
-                b = NT || k_ok ? w[i] : zero;      // several row tiles: dropped too (the ring, which has such jobs when they are more, fetches zeros)
+                b = k_ok ? w[i] : zero;      // dropped too: the ring, which has such jobs when they are more, fetches zeros
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -167,11 +167,11 @@ __device__ inline void dense_bf16_sums(const P &p, const Tile tile, float *lds, 
         for (; i + 3 < mine; i += 2) {
             // keep the instruction scheduler from sinking the loads below the next
             // multiply phase: each phase must stay where it is written
-            compute(w0, x0, ok0);
+            compute(w0, x0, TW || ok0);      // the last step of a wavefront, the only one that can end past K, is peeled
             __builtin_amdgcn_sched_barrier(0);
             load(step(i + 2), w0, x0, ok0);
             __builtin_amdgcn_sched_barrier(0);
-            compute(w1, x1, ok1);
+            compute(w1, x1, TW || ok1);
             __builtin_amdgcn_sched_barrier(0);
             load(step(i + 3), w1, x1, ok1);
             __builtin_amdgcn_sched_barrier(0);
@@ -191,7 +191,7 @@ __device__ inline void dense_bf16_sums(const P &p, const Tile tile, float *lds, 
         for (; i + 2 * D <= mine; i += D) {
 #pragma unroll
             for (int d = 0; d < D; ++d) {
-                compute(w[d], x[d], !NT || ok[d]);      // the last step of a wavefront, the only one that can end past K, is peeled
+                compute(w[d], x[d], TW || !NT || ok[d]);      // as above
                 __builtin_amdgcn_sched_barrier(0);
                 load(step(i + d + D), w[d], x[d], ok[d]);
                 __builtin_amdgcn_sched_barrier(0);
