@@ -227,7 +227,8 @@ int32_t dense_backward(salus_pool_t *pool, const salus_dense_grad_desc *descs, u
         char *dy = at.lane + d.dy_off, *work = at.lane + d.work_off, *dz = linear ? dy : work;      // dZ of a linear layer is dY
         slope.push_back({dy, linear ? nullptr : (const float *)(at.lane + d.z_off), linear ? nullptr : work, (float *)(work + up256(M * d.N * 2)),
                          (float *)at_or_null(at.lane, d.db_off), d.M, d.N, (uint32_t)d.act});
-        if (d.dx_off != SALUS_ABSENT) input.push_back({at.persist + d.w_off, dz, at.lane + d.dx_off, nullptr, nullptr, nullptr, d.M, d.N, d.K, kOutBf16});
+        if (d.dx_off != SALUS_ABSENT)
+            input.push_back({at.persist + d.w_off, dz, at.lane + d.dx_off, nullptr, nullptr, nullptr, d.M, d.N, d.K, kOutBf16});
         weight.push_back({at.lane + d.x_off, dz, at.lane + d.dw_off, d.M, d.K, d.N});
         return nullptr;
     });

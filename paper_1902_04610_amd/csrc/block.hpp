@@ -53,10 +53,10 @@ enum class Epilogue { kDense, kGated, kGateGrad, kPlainT };
 
 // ---- activations ------------------------------------------------------------------------------------------------------------
 // NaNs pass through all of them and their slopes, as they do through the products: a gradient of what is no number is none.
-// Upper tail of the normal distribution at c in [0, 9]: 2^p(c), p the polynomial of degree 8 that minimizes the largest c |2^p - Q| over [0, 6] (1e-8; fitted
-// by linear programming), so Phi is off by 1.3e-7.  GELU(z) is z Q for negative z and z - z Q for others: max(z, 0) - |z| Q, which subtracts nothing from a negative z's
-// small result.  (The library's erfc takes four times as long: 24 jobs x 1 - 128 rows, 1000 -> 3080, float results, 9 of 49 us.)  gelu_fast, two degrees less,
-// suffices where a bf16 is next.
+// Upper tail of the normal distribution at c in [0, 9]: 2^p(c), p the polynomial of degree 8 that minimizes the largest c |2^p - Q| over [0, 6]
+// (1e-8; fitted by linear programming), so Phi is off by 1.3e-7.  GELU(z) is z Q for negative z and z - z Q for others: max(z, 0) - |z| Q,
+// which subtracts nothing from a negative z's small result.  (The library's erfc takes four times as long: 24 jobs x 1 - 128 rows,
+// 1000 -> 3080, float results, 9 of 49 us.)  gelu_fast, two degrees less, suffices where a bf16 is next.
 __device__ inline float tail_exponent(float c)
 {
     float p = fmaf(-1.8847762248697109e-06f, c, 2.7810900064650923e-05f);
@@ -69,9 +69,10 @@ __device__ inline float tail_exponent(float c)
     return fmaf(p, c, -0.9999998211860657f);
 }
 __device__ inline float normal_tail(float c) { return __builtin_amdgcn_exp2f(tail_exponent(c)); }
-// The same at c in [0, 13] for results that stay floats: from 3.25 on, where an absolute error of Q is no small part of it any more, the polynomial of degree 7 that minimizes
-// the largest |p - log2 Q| over [3.25, 13].  GELU of it is off by less than 1.2e-7 of |z|, and for negative z by less than 2.1e-5 of itself down to -12.9, where it is 3e-37
-// (in float arithmetic).
+// The same at c in [0, 13] for results that stay floats: from 3.25 on, where an absolute error of Q is no small part of it any more, the polynomial
+// of degree 7 that minimizes the largest |p - log2 Q| over [3.25, 13].  GELU of it is off by less than 1.2e-7 of |z|, and for negative z by less
+// than 2.1e-5 of itself down to -12.9, where it is 3e-37 (in float arithmetic).  24 jobs x 1 - 128 rows as above, from the cache, 31.0 us with
+// one polynomial, 32.0 with both.
 __device__ inline float normal_tail_far(float c)
 {
     float p = fmaf(-6.624220816320303e-08f, c, 4.464800895220833e-06f);
@@ -83,7 +84,8 @@ __device__ inline float normal_tail_far(float c)
     p = fmaf(p, c, -1.106598138809204f);
     return __builtin_amdgcn_exp2f(c < 3.25f ? tail_exponent(c) : p);
 }
-// exp's argument is off by 2^-24 of itself, which the slope of the sigmoid takes back: 3e-8 of |z| at most in z sigmoid(z), beside the last bits of v_exp_f32 and v_rcp_f32.
+// exp's argument is off by 2^-24 of itself, which the slope of the sigmoid takes back: 3e-8 of |z| at most in z sigmoid(z), beside the last bits of
+// v_exp_f32 and v_rcp_f32.
 __device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
 __device__ inline float relu_nan(float z) { return z < 0.0f ? 0.0f : z; }
 
@@ -283,7 +285,9 @@ __device__ inline void finish_dense(const BlockProblem &p, const Part &at, uint3
         }
 }
 
-// act(g) * u of J blocks of each; g and u to Z, beside each other as they lie in the weights.
+// act(g) * u of J blocks of each; g and u to Z, beside each other as they lie in the weights.  The product is rounded to bf16 because it is a factor of
+// the second product, which the matrix pipes take as bf16: up to half a step, 2^-8, of each hidden activation, 1.7e-3 of the
+// results' size on average, as much as their own rounding.  g and u stay floats.
 template <int J>
 __device__ inline void finish_gated(const BlockProblem &p, const Part &at, uint32_t r0, uint32_t c0, const float (&g)[J][16],
                                     const float (&u)[J][16], int lane)
@@ -315,7 +319,7 @@ __device__ inline void finish_gated(const BlockProblem &p, const Part &at, uint3
     store_bf16<J>((uint16_t *)p.Y + (uint64_t)at.m * N + at.n, N, at, r0, c0, h, lane);
 }
 
-// dG = dH * u * act'(g) and dU = dH * act(g), beside each other, of J blocks of dH.  Eight rows at a time, the next eight asked for
+// dG = dH * u * act'(g) and dU = dH * act(g), beside each other, of J blocks of dH; rounded to bf16 as factors of dX and dWin.  Eight rows at a time, the next eight asked for
 // meanwhile: more of g and u does not fit beside the sums of a large tile.
 template <int J>
 __device__ inline void finish_gate_grad(const BlockProblem &p, const Part &at, uint32_t r0, uint32_t c0, const float (&v)[J][16], int lane)

@@ -68,8 +68,12 @@ struct Tiling {
     hipError_t (*launch)(const Round &);
     bool once = false;       // asks for weights non-temporally: for weights from HBM and calls that do not need them again
 };
-// Bytes per nanosecond, of weights from HBM, the most that tiles of fewer than 64 rows, other tiles, and tiles that ask non-temporally reached over the launches of more than 224 MB of weights.
-// 32 jobs x 1 - 32 rows, gated 1000 -> 2760 and dense 2760 -> 1000 (530 MB): 128-row tiles non-temporal / cached 111 / 120 us.
+// Bytes per nanosecond of weights from HBM: the most that tiles of fewer than 64 rows, other tiles, and tiles that ask non-temporally reached over the
+// launches of more than 224 MB of weights.  32 jobs x 1 - 32 rows, gated 1000 -> 2760 and dense 2760 -> 1000 (530 MB): 128-row tiles
+// non-temporal / cached 111 / 120 us.
+// Whether weights come from HBM is a guess by what is resident in the pool (weights_cached), float masters and jobs without a turn among it.  Where
+// it is wrong, weights that the cache holds beside 500 MB that no call touches, rounds take up to 1.15 of the time: 8 jobs x 128 rows,
+// 1024 -> 2736 -> 1024, 36.8 / 42.0 us, 32 x 100, 512 -> 1024 -> 512, 29.8 / 33.1, 8 x 64, 1024 -> 2736 -> 1024, 32.7 / 32.7.
 constexpr uint64_t kStreamNarrow = 4300, kStream = 4800, kStreamOnce = 5200;
 constexpr uint32_t kAnyRows = ~0u;
 
@@ -114,12 +118,14 @@ inline Choice choose(const Tiling (&tilings)[N], const BlockProblem *p, uint32_t
 template <int BM, int BN, int WM, int WN, int D, int PER_CU, Epilogue E>
 inline hipError_t ring(const Round &r)
 {
-    return launch_block<BlockArgs>(block_stream<BM, BN, WM, WN, D, PER_CU, E>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, PER_CU * resident_grid(), r.p, r.n, r.stream, r.launches);
+    return launch_block<BlockArgs>(block_stream<BM, BN, WM, WN, D, PER_CU, E>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, PER_CU * resident_grid(), r.p, r.n,
+                                   r.stream, r.launches);
 }
 template <int BM, int BN, int WM, int WN, int PER_CU, Epilogue E, bool ONCE = false>
 inline hipError_t tiled(const Round &r)
 {
-    return launch_block<BlockArgs>(block_tiled<BM, BN, WM, WN, E, ONCE>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, PER_CU * resident_grid(), r.p, r.n, r.stream, r.launches);
+    return launch_block<BlockArgs>(block_tiled<BM, BN, WM, WN, E, ONCE>, 64 * WM * WN, BM, BlockWalk<BM, BN, E>::kCols, PER_CU * resident_grid(), r.p, r.n,
+                                   r.stream, r.launches);
 }
 
 }  // namespace salus

@@ -141,23 +141,31 @@ static hipError_t narrow(const Round &r)
 {
     constexpr bool kGated = E == Epilogue::kGated;
     constexpr uint32_t kCols = kGated ? 8 * NB : 16 * NB;
-    if (r.n <= kBlockFew) return launch_block<BlockFewArgs>(block_narrow<MT, NB, TWO, kGated, BlockFewArgs>, kGemmThreads, 16 * MT, kCols, 0, r.p, r.n, r.stream, r.launches);
+    if (r.n <= kBlockFew)
+        return launch_block<BlockFewArgs>(block_narrow<MT, NB, TWO, kGated, BlockFewArgs>, kGemmThreads, 16 * MT, kCols, 0, r.p, r.n, r.stream, r.launches);
     return launch_block<BlockArgs>(block_narrow<MT, NB, TWO, kGated, BlockArgs>, kGemmThreads, 16 * MT, kCols, 0, r.p, r.n, r.stream, r.launches);
 }
 template <int MT, int CPL>
 static hipError_t narrow_grad(const Round &r)
 {
-    if (r.n <= kBlockFew) return launch_block<BlockFewArgs>(block_gate_grad_narrow<MT, CPL, BlockFewArgs>, kGemmThreads, 16 * MT, 16 * CPL, 0, r.p, r.n, r.stream, r.launches);
+    if (r.n <= kBlockFew)
+        return launch_block<BlockFewArgs>(block_gate_grad_narrow<MT, CPL, BlockFewArgs>, kGemmThreads, 16 * MT, 16 * CPL, 0, r.p, r.n, r.stream, r.launches);
     return launch_block<BlockArgs>(block_gate_grad_narrow<MT, CPL, BlockArgs>, kGemmThreads, 16 * MT, 16 * CPL, 0, r.p, r.n, r.stream, r.launches);
 }
-// Fitted to launches of drawn sizes (1 - 48 jobs of 1 - 4096 rows, widths of 64 - 8192; 210 dense, 105 gated, 61 gate gradients, 100 input gradients, kernel
-// traces of every kind of tile on each of them): off by 6 - 10 % in the median.  The choice is 1.9 % (dense), 2.7 % (gated) and 1.9 % (gate gradients) off the quickest kind on
-// average and 28, 33 and 34 % at most; the best single kind is 38 (64 x 64), 32 (64 x 128) and 25 % (32 x 32) off.  What each is for: narrow tiles fill the chip with few rows, the
-// ring streams weights past one or two row tiles, large tiles multiply.  1 job x 1 row, 4096 -> 1024: 16 columns 9.4 us, the ring 16; 32 jobs x 1 - 32 rows, 1000 -> 5520, 64 x 64 / 128 x 128 / 128 x 256
-// 75 / 73 / 73, 2760 -> 1000 37 / 37 / 55; 8 jobs x 64 rows, 2736 -> 1024, 32 x 64 / 64 x 64 20.7 / 25.8; 8 jobs x 1000 rows, 2048 -> 8192, 64 x 128 / 128 x 128 / 128 x 256 / 256 x 256 545 / 353 / 295 / 286.
-// The 64 x 64 ring: three workgroups of three stages on a compute unit, 0.99 of two of four over 27 drawn launches (0.90 - 1.0 above 512 tiles; fitted with two, and taken as 0.99 of that).
-// One 128 x 128 tile per compute unit: eight wavefronts instead of four, 4 jobs x 500 rows, 2048 -> 2048, 27.5 / 29.2 us, 2 x 2000, 1024 -> 1024, 18.3 / 19.7, 0.95 over 10 drawn launches of 130 - 256
-// tiles (gated and gate gradients: 0.98 - 1.04, not there); its time is set as the same share of the other's.
+// The times are fitted to launches of drawn sizes: 1 - 48 jobs of 1 - 4096 rows, widths of 64 - 8192; 210 dense, 105 gated, 61 gate gradients, 100 input
+// gradients, kernel traces of every kind of tile on each of them; off by 6 - 10 % in the median.  The choice is 1.9 % (dense), 2.7 % (gated) and
+// 1.9 % (gate gradients) off the quickest kind on average and 28, 33 and 34 % at most; the best single kind is 38 (64 x 64), 32 (64 x 128) and
+// 25 % (32 x 32) off.
+// What each is for: narrow tiles fill the chip with few rows, the ring streams weights past one or two row tiles, large tiles multiply.
+//   1 job x 1 row, 4096 -> 1024: 16 columns 9.4 us, the ring 16
+//   32 jobs x 1 - 32 rows, 1000 -> 5520: 64 x 64 75 us, 128 x 128 73, 128 x 256 73; 2760 -> 1000: 37, 37, 55
+//   8 jobs x 64 rows, 2736 -> 1024: 32 x 64 20.7 us, 64 x 64 25.8
+//   8 jobs x 1000 rows, 2048 -> 8192: 64 x 128 545 us, 128 x 128 353, 128 x 256 295, 256 x 256 286
+// The 64 x 64 ring has three workgroups of three stages on a compute unit and is listed with two, as what it was fitted with, two of four stages: it takes
+// 0.99 of their time over 27 drawn launches (0.90 - 1.0 above 512 tiles), which is how its numbers were scaled.
+// One 128 x 128 tile per compute unit: eight wavefronts instead of four, 4 jobs x 500 rows, 2048 -> 2048, 27.5 / 29.2 us, 2 x 2000, 1024 -> 1024,
+// 18.3 / 19.7, 0.95 over 10 drawn launches of 130 - 256 tiles (gated and gate gradients: 0.98 - 1.04, not there); its time is set as the same
+// share of the other's.
 constexpr Tiling kDense[] = {
     {16, 16, 1, 0, 16, 1300, 92, 1370, narrow<1, 1, false, Epilogue::kDense>},
     {32, 16, 1, 16, kAnyRows, 1300, 152, 1480, narrow<2, 1, false, Epilogue::kDense>},
@@ -209,7 +217,7 @@ hipError_t launch_block_gate_grad(const BlockProblem *p, uint32_t n, bool cached
 }
 
 // ---- slope of a dense layer -----------------------------------------------------------------------------------------------------
-// dZ = dY * act'(Z), and the column sums of dZ before its rounding.  A workgroup takes 16 rows of 512 columns, a wavefront four of the rows, a lane
+// dZ = dY * act'(Z), rounded to bf16 as a factor of dX and dW, and the column sums of dZ before its rounding.  A workgroup takes 16 rows of 512 columns, a wavefront four of the rows, a lane
 // eight columns; all of a lane's loads are on their way together.  The four wavefronts' sums are added in the order of the rows.  Bound by memory:
 // 8 bytes an element (2 and 4 read, 2 written).
 struct SlopeArgs {

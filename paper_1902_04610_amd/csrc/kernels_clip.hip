@@ -171,8 +171,8 @@ __device__ inline double clip_total(const ClipOwner &job)
 }
 
 // Vectors are as wide as the widest of what lies beside them allows to be read and written in whole lines: four elements with float weights.
-// PAST: what the call moves does not fit the memory-side cache, and goes past the caches (non-temporal): 8 jobs x 25 M elements, bf16 gradients, 455 / 482 us and the norms of the
-// next call, behind stores that are still under way, 71 / 124.
+// PAST: what the call moves does not fit the memory-side cache, and goes past the caches (non-temporal): 8 jobs x 25 M elements, bf16 gradients,
+// 455 / 482 us and the norms of the next call, behind stores that are still under way, 71 / 124.
 template <bool BF16, bool SGD, bool PAST>
 __device__ inline void apply_clip(const ClipChunk &k, float c, float lr)
 {

@@ -90,12 +90,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void weight_grad_tiled(WeightGradA
     T::run(walk, smem);
 }
 
-// Few rows: what bounds it is the writing of dW.  A wavefront owns 64 x 64 of dW, a workgroup four such blocks side by side.  Lane (c, g) loads the 8 x 4 blocks X[m + 8g ..][k0 +
-// 4c ..] and G[m + 8g ..][n0 + 4c ..] of a step of 32 rows, transposes them in registers into four A and four B operands of v_mfma_f32_16x16x32_bf16, and
-// ends up with 16 rows x 4 consecutive columns: 128 contiguous bytes per row across the 16 lanes.  What is wanted of up to 64 rows is asked for at once.
-// An XCD has a run of blocks down the rows of dW, which share their columns of G and, job by job, X in its L2, and three workgroups per compute unit: 8 jobs x 64 rows, 1024 -> 5472 and 2736 -> 1024
-// (134 MB of dW), 33.9 us, with blocks along the rows of dW dealt round-robin to the XCDs 43.9.  Four blocks below each other by one workgroup, G kept in registers: 31.7, but 1.4 of the time
-// on average over 25 launches of 1 - 96 rows.
+// Few rows: what bounds it is the writing of dW.  A wavefront owns 64 x 64 of dW, a workgroup four such blocks side by side.  Lane (c, g) loads the 8 x 4
+// blocks X[m + 8g ..][k0 + 4c ..] and G[m + 8g ..][n0 + 4c ..] of a step of 32 rows, transposes them in registers into four A and four B operands
+// of v_mfma_f32_16x16x32_bf16, and ends up with 16 rows x 4 consecutive columns: 128 contiguous bytes per row across the 16 lanes.  What is
+// wanted of up to 64 rows is asked for at once.
+// An XCD has a run of blocks down the rows of dW, which share their columns of G and, job by job, X in its L2, and three workgroups per compute unit:
+// 8 jobs x 64 rows, 1024 -> 5472 and 2736 -> 1024 (134 MB of dW), 33.9 us, with blocks along the rows of dW dealt round-robin to the XCDs 43.9.
+// Four blocks below each other by one workgroup, G kept in registers: 31.7, but 1.4 of the time on average over 25 launches of 1 - 96 rows.
 constexpr uint32_t kFewBlock = 64, kFewCols = 256, kFewSteps = 2;
 template <typename Args>
 __device__ inline void few_rows(const Args &a, uint32_t id)
@@ -197,8 +198,8 @@ __global__ __launch_bounds__(256) void block_column_sums(SumArgs a)
     column_sums(a, blockIdx.x, part);
 }
 
-// All three in a launch.  Few rows: input gradients through the ring, which few and long tiles of leave most of the chip's bandwidth, and weight gradients, which write.  More: 128 x 128
-// tiles of both, two workgroups per compute unit, one of which multiplies while the other begins or ends.
+// All three in a launch.  Few rows: input gradients through the ring, of which few and long tiles leave most of the chip's bandwidth, and weight
+// gradients, which write.  More: 128 x 128 tiles of both, two workgroups per compute unit, one of which multiplies while the other begins or ends.
 __global__ __launch_bounds__(256, 3) void gradients_few_rows(SharedArgs a)
 {
     using T = TileStream<64, 64, 2, 2, false, 3>;
@@ -305,9 +306,10 @@ constexpr Tiling kInputOther[] = {
     {64, 128, 2, 0, kAnyRows, 1400, 605, 2940, nullptr},
 };
 
-// Register blocks if a weight's rows, on average over the weights, are at most 96: 0.55 - 0.84 of the time of 128 x 128 tiles for up to 64 rows (32 launches of 0.1 - 140 MB of dW), 0.92 - 1.19 for 66 - 85,
-// 1.2 - 2.3 above 126.  Else 128 x 128 tiles, two per compute unit, or 256 x 256 ones, whichever should be quicker: 2 jobs x 4096 rows, 4096 -> 22016 and 11008 -> 4096, 3.09 and 1.92 ms, 4 jobs x 500,
-// 2048 -> 2048, 24.5 / 23.0 us.  (Over 100 launches of 1 - 4096 rows the choice between these two is 0.6 % off the quicker one.)
+// Register blocks if a weight's rows, on average over the weights, are at most 96: 0.55 - 0.84 of the time of 128 x 128 tiles for up to 64 rows (32 launches
+// of 0.1 - 140 MB of dW), 0.92 - 1.19 for 66 - 85, 1.2 - 2.3 above 126.  Else 128 x 128 tiles, two per compute unit, or 256 x 256 ones, whichever
+// should be quicker: 2 jobs x 4096 rows, 4096 -> 22016 and 11008 -> 4096, 3.09 and 1.92 ms, 4 jobs x 500, 2048 -> 2048, 24.5 / 23.0 us.  (Over 100
+// launches of 1 - 4096 rows the choice between these two is 0.6 % off the quicker one.)
 constexpr double kFewRows = 96;
 
 static bool rows_are_few(const WeightGradProblem *p, uint32_t n)
@@ -372,11 +374,13 @@ static SharedTiles shared_tiles(const BlockProblem *input, uint32_t n_input, con
     return s;
 }
 
-// Do input and weight gradients share a launch of 128 x 128 tiles?  Its time, from the tiles' as they run two on a compute unit: the longest tile, or all of them over all places and a quarter of
-// the longest for the end, of which a sixteenth is taken off: they measured that much quicker than this says; against the quickest launches of their own and 1.2 us for each that is saved (a launch
-// that adds columns: 3.5).  Training calls of drawn sizes: 0.90 of the time where this shares; over 43 of them 0.97 if
-// always shared, with 0.66 - 1.47 at the ends: 5 jobs x 125 - 262 rows, 704 -> 112, 18.9 / 28.4 us, 1 job x 486 rows, depth 14224, whose few input gradient tiles one compute unit walks alone,
-// 197 / 134.  4 jobs x 500 rows, 2048 -> 2048: 43.9, alone 4.6 + 22.2 + 23.4.
+// Do input and weight gradients share a launch of 128 x 128 tiles?  If its time is below that of the quickest launches of their own and 1.2 us for each
+// launch that is saved (one that adds columns: 3.5).  Its time, from the tiles' as they run two on a compute unit: the longest tile, or all of them
+// over all places and a quarter of the longest for the end; less a sixteenth, as they measured that much quicker than this says.
+// Training calls of drawn sizes: 0.90 of the time where this shares; over 43 of them 0.97 if always shared, with 0.66 - 1.47 at the ends.
+//   4 jobs x 500 rows, 2048 -> 2048: 43.9 us, alone 4.6 + 22.2 + 23.4
+//   5 jobs x 125 - 262 rows, 704 -> 112: 18.9, alone 28.4
+//   1 job x 486 rows, depth 14224, whose few input gradient tiles one compute unit walks alone: 197, alone 134
 static bool share_tiled(const BlockProblem *input, uint32_t n_input, const WeightGradProblem *weight, uint32_t n_weight, bool sums)
 {
     const SharedTiles s = shared_tiles(input, n_input, weight, n_weight);
@@ -389,10 +393,15 @@ static bool share_tiled(const BlockProblem *input, uint32_t n_input, const Weigh
     return shared - shared / 16 < alone + 1200 + (sums ? 3500 : 0);
 }
 
-// And a launch of ring tiles and register blocks?  Beside the writes an input gradient's tile takes up to twice as long: worth it unless that is what the launch lasts.  More than 16 rows: depth up to 4096, or any where
-// dW is at most 64 MB; fewer, whose narrow tiles alone are quicker: depth up to 2048, or 4096 where there are half as many tiles as compute units.  83 training calls of drawn sizes, of which 45 are of few rows: 0.87
-// of the time on average where this shares.  7 jobs x 13 - 23 rows, depth 3232, 24.6 us, alone 2.8 + 11.7 + 11.8 + 14.7; 3 jobs x 45 - 49 rows, 3696, 25.0, alone 17.9 + 14.9; 2 jobs x 19 - 21 rows, 8032 (53 MB), 36.8, alone
-// 29.2 + 13.3; 8 jobs x 64 rows, 5472 (134 MB), 69, alone 25 + 34; 1 job x 13 rows, 4256, 21.3, alone 12.5 + 6.0.
+// And a launch of ring tiles and register blocks?  Beside the writes an input gradient's tile takes up to twice as long: worth it unless that is what the
+// launch lasts.  More than 16 rows: depth up to 4096, or any where dW is at most 64 MB; fewer, whose narrow tiles alone are quicker: depth up to
+// 2048, or 4096 where there are half as many tiles as compute units.
+// 83 training calls of drawn sizes, of which 45 are of few rows: 0.87 of the time on average where this shares.
+//   7 jobs x 13 - 23 rows, depth 3232: 24.6 us, alone 2.8 + 11.7 + 11.8 + 14.7
+//   3 jobs x 45 - 49 rows, 3696: 25.0, alone 17.9 + 14.9
+//   2 jobs x 19 - 21 rows, 8032 (53 MB): 36.8, alone 29.2 + 13.3
+//   8 jobs x 64 rows, 5472 (134 MB): 69, alone 25 + 34
+//   1 job x 13 rows, 4256: 21.3, alone 12.5 + 6.0
 static bool share_few_rows(const BlockProblem *input, uint32_t n_input, const WeightGradProblem *weight, uint32_t n_weight)
 {
     uint64_t bytes = 0, tiles = 0;
@@ -423,12 +432,16 @@ hipError_t launch_gradients(const BlockProblem *input, uint32_t n_input, const W
             a.weights = (uint32_t)out;
             hipLaunchKernelGGL(gradients_few_rows, dim3(a.sums + a.inputs + a.weights), dim3(256), 0, stream, a);
         } else {
-            // All of them have a place, or places (a multiple of 8 for the XCDs) go by the work, unless whole tiles fall much better otherwise: by the time of the kind whose workgroups take longer and a
-            // quarter of the other's, a fifth less.  4 jobs x 500 rows, 2048 -> 2048, 256 and 1024 tiles, on 256 and 256 places 43.9 us, on 232 and 280 48.6; 10 x 400, 768 -> 768, 240 and 360 tiles, 21 / 23.4.
-            // Where the formula says less it is wrong as often as right: 9 jobs x 204 - 249 rows, 3280 -> 400, 14 % by the formula, 26.5 / 25.0; 13 jobs x 490, 12 %, 793 / 845.
+            // All of them have a place.  Else places (a multiple of 8 for the XCDs) go by the work, unless whole tiles fall much better otherwise: by
+            // the time of the kind whose workgroups take longer and a quarter of the other's, a fifth less.
+            //   4 jobs x 500 rows, 2048 -> 2048, 256 and 1024 tiles: 43.9 us on 256 and 256 places, 48.6 on 232 and 280
+            //   10 x 400, 768 -> 768, 240 and 360 tiles: 21 / 23.4
+            // Where the formula says less it is wrong as often as right: 9 jobs x 204 - 249 rows, 3280 -> 400, 14 % by the formula, 26.5 / 25.0;
+            // 13 jobs x 490, 12 %, 793 / 845.
             uint64_t most = in;
             if (in + out > places) {
-                const uint64_t x = shared_tiles(input, n_input, nullptr, 0).work / in, y = shared_tiles(nullptr, 0, weight, n_weight).work / out;      // of a tile, two on a compute unit
+                // of a tile, two on a compute unit
+                const uint64_t x = shared_tiles(input, n_input, nullptr, 0).work / in, y = shared_tiles(nullptr, 0, weight, n_weight).work / out;
                 auto ns = [&](uint64_t i) {
                     const uint64_t i_ns = (in + i - 1) / i * x, w_ns = (out + places - i - 1) / (places - i) * y;
                     return std::max(i_ns, w_ns) + std::min(i_ns, w_ns) / 4;
