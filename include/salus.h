@@ -428,6 +428,91 @@ uint64_t salus_clip_work_bytes(const salus_clip_tensor *tensors, uint32_t n_tens
 int32_t salus_grouped_clip(salus_pool_t *pool, const salus_clip_desc *descs, uint32_t n, void *stream);
 int32_t salus_grouped_clip_sgd(salus_pool_t *pool, const salus_clip_desc *descs, uint32_t n, void *stream);
 
+/* ---- answering: a paged cache of keys and values, attention over it, tokens from logits --------
+ * What a packed round of language models that answer does between its dense layers, as packed calls under the rules of the transformer blocks
+ * above: all n jobs together on `stream`, asynchronously, recordable in a graph; inputs and caches are bf16, sums float (sampling: 64 bits); a
+ * result does not depend on the other jobs' data, nor on atomics.
+ *
+ * A job's cache lies in its persistent block, so that it moves and leaves with the job: n_pages pages of `page` tokens (a power of two,
+ * 32 - 1024) for Hkv heads of D elements (32, 64, 96, 128, 192 or 256), keys at k_off and values at v_off, 2 n_pages Hkv page D bytes each
+ * (salus_cache_bytes).  Element d of token t of page p and head h lies, in elements from the beginning,
+ *     keys     at (p Hkv + h) page D + ((t / 32) (D / 8) + d / 8) 256 + (t % 32) 8 + d % 8
+ *     values   at (p Hkv + h) page D + ((t / 8) D + d) 8 + t % 8,
+ * the order in which the matrix pipes take them.  A page may be copied as a whole.
+ *
+ * The new rows of a round and the sequences they belong to lie in the job's lane as int32 arrays, read on the device (a recorded call takes
+ * what they hold when it is replayed): starts, n_seqs + 1 entries that do not fall, sequence s has rows starts[s] .. starts[s + 1] - 1 of M (none
+ * is fine; M Hq + 32 n_seqs Hkv is below 2^31); lens, its tokens with the new ones, so that its n rows are its last n tokens; table, max_pages entries a sequence, the page
+ * of token t is table[s][t / page].  Entries behind a sequence's last page are not used.  Rows in no sequence are neither read nor written.  What a device array
+ * should not hold is harmless: rows outside 0 .. M are left out, tokens in pages outside 0 .. n_pages - 1 are neither stored nor seen,
+ * rows in front of token 0 are not stored and see nothing. */
+
+/* Bytes of the keys, or of the values, of a cache; 0 if there is no such cache. */
+uint64_t salus_cache_bytes(uint32_t n_pages, uint32_t Hkv, uint32_t page, uint32_t D);
+
+enum { SALUS_ROTARY_HALF = 0,           /* pair j of a head: elements j and j + rotary / 2 */
+       SALUS_ROTARY_INTERLEAVED = 1 };  /* elements 2 j and 2 j + 1 */
+
+/* Frequencies of the position rotation, radians a token, of pair j of rotary / 2: f = base^(-2 j / rotary), for contexts longer than the trained
+ * ones slowed down.  LINEAR: f / factor.  BASE: base factor^(rotary / (rotary - 2)) in place of base (the last pair is slowed by factor, the first
+ * not; rotary 2 has one pair only and keeps it).  PARTS: pairs that turn at most `slow` times in `trained` tokens are slowed by factor, those that turn at least `fast` times are not, with
+ * r f + (1 - r) f / factor between, r = (turns - slow) / (fast - slow).  `trained`, slow and fast are used by PARTS alone.  Host
+ * function; SALUS_EINVAL unless rotary is even, positive and at most 256, base > 1, factor >= 1 and, for PARTS, trained > 0 and 0 <= slow < fast, all finite. */
+enum { SALUS_ROTARY_PLAIN = 0, SALUS_ROTARY_LINEAR = 1, SALUS_ROTARY_BASE = 2, SALUS_ROTARY_PARTS = 3 };
+int32_t salus_rotary_frequencies(double *out, uint32_t rotary, double base, int32_t scaling, double factor, double trained,
+                                 double slow, double fast);
+
+/* Rotates the new rows' queries and keys by their positions and stores keys and values in the cache.  x: M x (Hq + 2 Hkv) D bf16 in the lane, a row's
+ * query heads in front of its key heads in front of its value heads, as one product makes them; q: M x Hq D bf16, written.  Of each query and key head the first
+ * `rotary` elements (even, at most D, 0: none) turn, the pair (a, b) of frequency f at position p into
+ *     m (a cos(p f) - b sin(p f)),  m (a sin(p f) + b cos(p f)),     m = magnitude (finite; 1 unless the scaling wants another),
+ * angles in 64 bits; the rest and the values are copied.  freq: rotary / 2 doubles in the persistent block (SALUS_ABSENT exactly if rotary is 0).
+ * Two rows must not be stored in the same place (sequences that share a page append to pages of their own). */
+typedef struct {
+    int32_t  job;
+    uint32_t M, n_seqs, Hq, Hkv, D, page, n_pages, max_pages;
+    uint32_t rotary;
+    int32_t  layout;       /* SALUS_ROTARY_HALF or SALUS_ROTARY_INTERLEAVED */
+    float    magnitude;
+    uint64_t k_off, v_off, freq_off;
+    uint64_t x_off, q_off, starts_off, lens_off, table_off;
+} salus_append_desc;
+int32_t salus_grouped_append(salus_pool_t *pool, const salus_append_desc *descs, uint32_t n, void *stream);
+
+/* Attention of the new rows over the cache, to which they have been appended: for query head h of a row at position p, with key head h / (Hq / Hkv),
+ *     y = sum_t w_t v_t / sum_t w_t,   w_t = exp(scale q . k_t),   over tokens t <= p, with a window only p - window < t,
+ * zero if it sees none.  A token that a row does not see does not reach it, whatever its key and value hold.  q, y: M x Hq D bf16 in the lane; scale positive and
+ * finite; window 0: none.  Weights are rounded to bf16 as factors of the second product; a score beyond the largest float is none.  max_len: no sequence of the round is longer (longer ones are taken as of that
+ * length); it bounds the launch, so that one recorded with max_len = max_pages page serves all lengths.  work:
+ * salus_attention_work_bytes() (0: work_off is ignored).  max_len is below 2^30. */
+typedef struct {
+    int32_t  job;
+    uint32_t M, n_seqs, Hq, Hkv, D, page, n_pages, max_pages;
+    uint32_t max_len, window;
+    float    scale;
+    uint64_t k_off, v_off;
+    uint64_t q_off, y_off, starts_off, lens_off, table_off, work_off;
+} salus_attention_desc;
+uint64_t salus_attention_work_bytes(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len);
+int32_t salus_grouped_attention(salus_pool_t *pool, const salus_attention_desc *descs, uint32_t n, void *stream);
+
+/* One token from each of M rows of V logits (M x ld in the lane, float or bf16, ld a multiple of 8 and at least V; what follows a row's V logits is not used).  Tokens are
+ * ordered by logit, equal ones by index.  A row's parameters are params[4 r ..]: float temperature, int32 top_k, float top_p, float min_p; u[r], in [0, 1),
+ * is its random number.  With w = exp((logit - largest) / temperature), kept are of that order
+ *     the first top_k (0 and below: all),  of these the fewest from the front whose w reach top_p of their sum,  of these those with w >= min_p,
+ * at least the first, and the token is the smallest index up to which the sum of the kept w, in order of index, exceeds u times the sum of all kept.  Temperature 0 and below (or NaN): the first
+ * of the order.  top_p of 1 and above or NaN, min_p of 0 and below or NaN: no limit; u is cut to [0, 1).  A NaN counts as minus infinity; where nothing is larger, the token is -1.
+ * Weights are in 64 bits and count in steps of 2^-44 of the largest, whose sums do not depend on any order.  tokens: M int32, written. work:
+ * salus_sample_work_bytes().  V is at least 1 and at most 2^19. */
+typedef struct {
+    int32_t  job;
+    uint32_t M, V, ld;
+    int32_t  dtype;        /* SALUS_F32 or SALUS_BF16: of the logits */
+    uint64_t logits_off, params_off, u_off, tokens_off, work_off;
+} salus_sample_desc;
+uint64_t salus_sample_work_bytes(uint32_t M, uint32_t V);
+int32_t salus_grouped_sample(salus_pool_t *pool, const salus_sample_desc *descs, uint32_t n, void *stream);
+
 /* Efficient job switching made explicit for jobs that cannot stay
  * (Sections 3.2 and 4.2): RESIDENT -> EVICTED copies the persistent block to
  * pinned host memory and frees it.  pinned_or_null: caller-owned pinned,

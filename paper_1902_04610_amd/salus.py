@@ -21,6 +21,8 @@ ABSENT = 2 ** 64 - 1              # an offset that is not given
 F32, BF16 = 0, 1
 COPY_KERNEL, COPY_DMA = 0, 1
 LAYOUT_ROWMAJOR, LAYOUT_STRIP128 = 0, 1
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
 FLAG_SHRINK_LANES = 1
 FLAG_FUSE_DEPTHS = 2
 
@@ -107,6 +109,24 @@ class ClipDesc(C.Structure):
                 ("max_norm", C.c_float), ("lr", C.c_float), ("norm_off", C.c_uint64), ("work_off", C.c_uint64)]
 
 
+_CACHED = [("job", C.c_int32)] + [(name, C.c_uint32) for name in "M n_seqs Hq Hkv D page n_pages max_pages".split()]
+
+
+class AppendDesc(C.Structure):
+    _fields_ = _fields(_CACHED + [("rotary", C.c_uint32), ("layout", C.c_int32), ("magnitude", C.c_float)],
+                       "k_off v_off freq_off x_off q_off starts_off lens_off table_off")
+
+
+class AttentionDesc(C.Structure):
+    _fields_ = _fields(_CACHED + [("max_len", C.c_uint32), ("window", C.c_uint32), ("scale", C.c_float)],
+                       "k_off v_off q_off y_off starts_off lens_off table_off work_off")
+
+
+class SampleDesc(C.Structure):
+    _fields_ = _fields([("job", C.c_int32), ("M", C.c_uint32), ("V", C.c_uint32), ("ld", C.c_uint32), ("dtype", C.c_int32)],
+                       "logits_off params_off u_off tokens_off work_off")
+
+
 class Stats(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in (
         "rounds", "iterations", "bytes_d2h", "bytes_h2d", "bytes_d2d", "moves", "compactions",
@@ -148,6 +168,13 @@ _PROTOS = {
     "salus_grouped_clip": [C.c_void_p, C.POINTER(ClipDesc), C.c_uint32, C.c_void_p],
     "salus_grouped_clip_sgd": [C.c_void_p, C.POINTER(ClipDesc), C.c_uint32, C.c_void_p],
     "salus_clip_work_bytes": [C.POINTER(ClipTensor), C.c_uint32],
+    "salus_cache_bytes": [C.c_uint32] * 4,
+    "salus_rotary_frequencies": [C.POINTER(C.c_double), C.c_uint32, C.c_double, C.c_int32] + [C.c_double] * 4,
+    "salus_grouped_append": [C.c_void_p, C.POINTER(AppendDesc), C.c_uint32, C.c_void_p],
+    "salus_grouped_attention": [C.c_void_p, C.POINTER(AttentionDesc), C.c_uint32, C.c_void_p],
+    "salus_attention_work_bytes": [C.c_uint32] * 6,
+    "salus_grouped_sample": [C.c_void_p, C.POINTER(SampleDesc), C.c_uint32, C.c_void_p],
+    "salus_sample_work_bytes": [C.c_uint32] * 2,
     "salus_switch_out": [C.c_void_p, C.c_int32, C.c_void_p],
     "salus_switch_in": [C.c_void_p, C.c_int32],
     "salus_switch_out_begin": [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p],
@@ -186,7 +213,7 @@ def lib():
             fn = getattr(L, name)
             fn.argtypes = args
             fn.restype = (C.c_char_p if name == "salus_last_error" else
-                          C.c_uint64 if name.endswith("_work_bytes") else C.c_int32)
+                          C.c_uint64 if name.endswith("_bytes") else C.c_int32)
         _lib = L
     return _lib
 
@@ -380,6 +407,23 @@ class Pool:
                                         for it, t in zip(items, keep)])
         return arr, keep
 
+    @staticmethod
+    def make_append_descs(items):
+        """dicts(job, M, n_seqs, Hq, Hkv, D, page, n_pages, max_pages, rotary, layout, magnitude, k_off, v_off[, freq_off], x_off, q_off, starts_off,
+        lens_off, table_off)"""
+        return Pool._make(AppendDesc, items)
+
+    @staticmethod
+    def make_attention_descs(items):
+        """dicts(job, M, n_seqs, Hq, Hkv, D, page, n_pages, max_pages, max_len, window, scale, k_off, v_off, q_off, y_off, starts_off, lens_off,
+        table_off[, work_off])"""
+        return Pool._make(AttentionDesc, items)
+
+    @staticmethod
+    def make_sample_descs(items):
+        """dicts(job, M, V, ld, dtype, logits_off, params_off, u_off, tokens_off, work_off)"""
+        return Pool._make(SampleDesc, items)
+
     def _grouped(self, call, descs, n, stream):
         if n is not None and not 0 <= n <= len(descs):
             raise ValueError(f"n is {n}, of {len(descs)} descriptors")
@@ -403,6 +447,15 @@ class Pool:
 
     def grouped_clip_sgd(self, descs, n=None, stream=None):
         return self._grouped("salus_grouped_clip_sgd", descs, n, stream)
+
+    def grouped_append(self, descs, n=None, stream=None):
+        return self._grouped("salus_grouped_append", descs, n, stream)
+
+    def grouped_attention(self, descs, n=None, stream=None):
+        return self._grouped("salus_grouped_attention", descs, n, stream)
+
+    def grouped_sample(self, descs, n=None, stream=None):
+        return self._grouped("salus_grouped_sample", descs, n, stream)
 
     # -- switching -----------------------------------------------------------------
     def switch_out(self, job, pinned_ptr=None):
@@ -485,6 +538,32 @@ def _clip_tensors(tensors):
 def clip_work_bytes(tensors):
     """tensors: the dicts of make_clip_descs (only counts matter)"""
     return lib().salus_clip_work_bytes(_clip_tensors(tensors), len(tensors))
+
+
+def _whole(**sizes):
+    return [_fits(C.c_uint32, name, value) for name, value in sizes.items()]
+
+
+def cache_bytes(n_pages, Hkv, page, D):
+    """Bytes of the keys, or of the values, of a paged cache."""
+    return lib().salus_cache_bytes(*_whole(n_pages=n_pages, Hkv=Hkv, page=page, D=D))
+
+
+def attention_work_bytes(M, n_seqs, Hq, Hkv, D, max_len):
+    return lib().salus_attention_work_bytes(*_whole(M=M, n_seqs=n_seqs, Hq=Hq, Hkv=Hkv, D=D, max_len=max_len))
+
+
+def sample_work_bytes(M, V):
+    return lib().salus_sample_work_bytes(*_whole(M=M, V=V))
+
+
+def rotary_frequencies(rotary, base=10000.0, scaling=ROTARY_PLAIN, factor=1.0, trained=4096.0, slow=1.0, fast=32.0):
+    """rotary / 2 frequencies, radians a token, as a list of floats."""
+    out = (C.c_double * max(1, rotary // 2))()
+    rc = lib().salus_rotary_frequencies(out, _fits(C.c_uint32, "rotary", rotary), base, scaling, factor, trained, slow, fast)
+    if rc != OK:
+        raise SalusError(rc, "salus_rotary_frequencies")
+    return list(out)
 
 
 def scan_u64(values, scratch_ptr, stream=None):
