@@ -5,42 +5,104 @@
 //   token: the smallest index up to which the sum of the kept w exceeds u times the sum of all kept
 //
 // Every limit keeps a beginning of the order, so nothing is sorted: the place of a token in the order is a 52-bit number (the logit's bits, made
-// monotonous, in front of the index), and a limit is the number of the last token that is kept, found eleven bits at a time by histograms of how many tokens
-// there are, or how much weight.  Weights are 64-bit exponentials, counted as whole multiples of 2^-44: their sums are the same in any order,
-// so that atomic additions do not show, and off by less than 2^-25 of the largest weight for 2^19 tokens.
+// monotonous, in front of the index), and a limit is the number of the last token that is kept.
+//
+// Bound by reading the logits, once.  Two kernels:
+//   slice_rows    a workgroup takes 8192 logits of a row and leaves their first token, their sum of weights if the row wants it, and the places of
+//                 those that a limit may keep, in order of index: all down to a threshold that at least so many of its threads' largest logits reach as
+//                 the limit may want of one slice; for top_p also the weight in bins of 1 / 16 of a power of two.
+//   choose_rows   a workgroup per row puts that together.  Without limits it reads one slice again; where the kept tokens all lie above every
+//                 slice's threshold, which the lists tell, none.  Else it finds the bin in which top_p ends, reads the row once for the kept weight of sixteen
+//                 runs of it and for that bin's tokens, and one run again for the token.
+// What even that does not hold (lists that run over: thousands of equal logits, top_k beyond them) is found by reading the row several times
+// (choose_anywhere), eleven bits of the last place at a time by histograms of how many tokens there are, or how much weight.
+//
+// Weights are 64-bit exponentials of differences to the row's largest logit; where they are summed by atomic additions they count as whole multiples of 2^-44, so that
+// no order shows.
+#include <cfloat>
+
 #include "answer.hpp"
 
 namespace salus {
 
 constexpr uint32_t kSampleThreads = 1024, kSampleWaves = kSampleThreads / 64, kBins = 2048;
 constexpr double kWeightUnit = 17592186044416.0;      // 2^44
+constexpr uint32_t kSliceThreads = 512, kSliceWaves = kSliceThreads / 64, kSlice = 8192, kListed = 64, kMostListed = 4096, kMassBins = 512;
 
-// Units of eight logits of a row.
-template <bool BF16>
+// What slice_rows leaves of a slice.
+struct Slice {
+    uint64_t first;          // place of its first token, 0 if it has none
+    double mass;             // sum of its weights relative to its first token's
+    uint32_t count[kSliceWaves];      // tokens of its wavefronts' lists; more than kListed: the list has not all
+    uint32_t down_to;        // the lists have all whose logit's bits (the upper 32 of a place) reach this
+    int32_t bin;             // of its first token, if its weights are in bins
+    uint32_t binned;
+    uint32_t pad;
+};
+typedef uint32_t SliceWords __attribute__((ext_vector_type(4)));
+constexpr uint32_t kSliceWords = sizeof(Slice) / sizeof(SliceWords);
+static_assert(kSliceWaves == 8 && kSliceWords == 4, "stored as words");
+
+// Work of a row: its slices, their lists of kListed places for each wavefront, their bins.
+__host__ __device__ inline uint32_t slices_of(uint32_t V) { return (V + kSlice - 1) / kSlice; }
+struct RowWork {
+    Global<char> *at;
+    uint32_t slices, units;      // slices, units of each (fewer of the last)
+    __host__ __device__ static uint64_t size(uint32_t V) { return (uint64_t)slices_of(V) * (sizeof(Slice) + 8 * kSliceWaves * kListed + 8 * kMassBins); }
+    __device__ RowWork(const SampleProblem &p, uint32_t r) : at((Global<char> *)p.work + r * size(p.V)), slices(slices_of(p.V)), units(((p.V + 7) / 8 + slices - 1) / slices) {}
+    __device__ Global<SliceWords> *slice(uint32_t i) const { return (Global<SliceWords> *)at + kSliceWords * i; }
+    __device__ Global<uint64_t> *list(uint32_t i, uint32_t wave) const { return (Global<uint64_t> *)slice(slices) + (i * kSliceWaves + wave) * kListed; }
+    __device__ Global<uint64_t> *bins(uint32_t i) const { return list(slices, 0) + i * kMassBins; }
+    __device__ void store(uint32_t i, const Slice &s) const
+    {
+        Global<SliceWords> *to = slice(i);
+        const uint64_t mass = __builtin_bit_cast(uint64_t, s.mass);
+        to[0] = SliceWords{(uint32_t)s.first, (uint32_t)(s.first >> 32), (uint32_t)mass, (uint32_t)(mass >> 32)};
+        to[1] = SliceWords{s.count[0], s.count[1], s.count[2], s.count[3]};
+        to[2] = SliceWords{s.count[4], s.count[5], s.count[6], s.count[7]};
+        to[3] = SliceWords{s.down_to, (uint32_t)s.bin, s.binned, 0};
+    }
+    __device__ Slice load(uint32_t i) const
+    {
+        const Global<SliceWords> *from = slice(i);
+        const SliceWords a = from[0], b = from[1], c = from[2], d = from[3];
+        return {(uint64_t)a[1] << 32 | a[0], __builtin_bit_cast(double, (uint64_t)a[3] << 32 | a[2]), {b[0], b[1], b[2], b[3], c[0], c[1], c[2], c[3]}, d[0], (int32_t)d[1], d[2], 0};
+    }
+};
+
+// A row's logits.  What is no number becomes minus infinity (of a number and NaN the larger is the number), minus zero becomes zero.
 struct LogitRow {
     const Global<char> *at;
-    uint32_t V;
+    uint32_t V, bf16;
+    __device__ LogitRow(const SampleProblem &p, uint32_t r) : at((const Global<char> *)p.logits + (uint64_t)r * p.ld * (p.bf16 ? 2 : 4)), V(p.V), bf16(p.bf16) {}
     __device__ uint32_t units() const { return (V + 7) / 8; }
-    // What is no logit, and NaN, become minus infinity; minus zero becomes zero.
-    __device__ void load(uint32_t unit, float (&x)[8]) const
+    __device__ static float clean(float x) { return fmaxf(x, -INFINITY) + 0.0f; }
+    __device__ float operator[](uint32_t i) const
     {
-        if constexpr (BF16) {
-            const u32x4 w = *(const Global<u32x4> *)(at + (uint64_t)unit * 16);
+        return clean(bf16 ? bf16_low(((const Global<uint16_t> *)at)[i]) : ((const Global<float> *)at)[i]);
+    }
+    // Eight of them.
+    struct Raw { u32x4 w[2]; };
+    __device__ Raw raw(uint32_t unit) const
+    {
+        Raw r;
+        r.w[0] = *(const Global<u32x4> *)(at + (uint64_t)unit * (bf16 ? 16 : 32));
+        if (!bf16) r.w[1] = *(const Global<u32x4> *)(at + (uint64_t)unit * 32 + 16);
+        return r;
+    }
+    __device__ void convert(const Raw &r, uint32_t unit, float (&x)[8]) const
+    {
+        if (bf16) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * i] = bf16_low(w[i]);
-                x[2 * i + 1] = bf16_high(w[i]);
-            }
+            for (int i = 0; i < 8; ++i) x[i] = clean(i % 2 ? bf16_high(r.w[0][i / 2]) : bf16_low(r.w[0][i / 2]));
         } else {
-            const f32x4 a = *(const Global<f32x4> *)(at + (uint64_t)unit * 32), b = *(const Global<f32x4> *)(at + (uint64_t)unit * 32 + 16);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[i] = a[i];
-                x[4 + i] = b[i];
-            }
+            for (int i = 0; i < 8; ++i) x[i] = clean(as_float(r.w[i / 4][i % 4]));
         }
+        if (unit * 8 + 8 > V) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = unit * 8 + i < V && x[i] == x[i] ? x[i] + 0.0f : -INFINITY;
+            for (int i = 0; i < 8; ++i) x[i] = unit * 8 + i < V ? x[i] : -INFINITY;
+        }
     }
 };
 
@@ -58,26 +120,49 @@ __device__ inline float logit_of(uint64_t place)
     return __builtin_bit_cast(float, b & 0x80000000u ? b & 0x7fffffffu : ~b);
 }
 
-__device__ inline uint64_t wave_max_u64(uint64_t v)
+__device__ inline uint32_t key_of(float x)
 {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v = max(v, (uint64_t)__shfl_xor((unsigned long long)v, d, 64));
-    return v;
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ inline uint64_t wave_sum_u64(uint64_t v)
+__device__ inline float float_of(uint32_t key) { return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+
+// 2^(d per), the product from -64 to 0, to 1e-11 of itself: the series of 2^f = e^(f ln 2) up to f^9 on [-1/2, 1/2], whose next term is below (ln 2 / 2)^10 / 10! = 7e-12;
+// 3 2^51 rounds to whole numbers, which then stand in the lowest bits.
+__device__ inline double power_of_two(double d, double per)
 {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor((unsigned long long)v, d, 64);
-    return v;
+    constexpr double kWhole = 6755399441055744.0, kLn2 = 0.6931471805599453, k2 = kLn2 * kLn2, k4 = k2 * k2;
+    const double whole = fma(d, per, kWhole), f = fma(d, per, kWhole - whole);
+    double v = fma(k4 * k4 * kLn2 / 362880, f, k4 * k4 / 40320);
+    v = fma(v, f, k4 * k2 * kLn2 / 5040);
+    v = fma(v, f, k4 * k2 / 720);
+    v = fma(v, f, k4 * kLn2 / 120);
+    v = fma(v, f, k4 / 24);
+    v = fma(v, f, k2 * kLn2 / 6);
+    v = fma(v, f, k2 / 2);
+    v = fma(v, f, kLn2);
+    v = fma(v, f, 1.0);
+    return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, v) + (__builtin_bit_cast(uint64_t, whole) << 52));
 }
 
-struct RowLimits {
-    float top;                   // largest logit
-    double per_temperature;
+// Weights relative to a row's, or a slice's, largest logit.
+struct Weights {
+    float top;
+    double per;              // log2(e) / temperature
+    __device__ Weights(float t, float temperature) : top(t), per(1.4426950408889634 / (double)temperature) {}
+    __device__ double of(float x) const
+    {
+        const double d = (double)x - (double)top;
+        return x == top ? 1.0 : top == INFINITY || !(d * per > -64.0) ? 0.0 : power_of_two(d, per);
+    }
+};
+
+struct RowLimits : Weights {
     uint64_t first;              // place of the first token
     uint64_t cut;                // place of the last token that is kept by top_k and top_p
     double min_p;
-    __device__ double weight(float x) const { return x == top ? 1.0 : top == INFINITY ? 0.0 : exp(((double)x - (double)top) * per_temperature); }
+    __device__ RowLimits(uint64_t first_place, float temperature, float min) : Weights(logit_of(first_place), temperature), first(first_place), cut(0), min_p((double)min) {}
+    __device__ double weight(float x) const { return of(x); }
     __device__ uint64_t units(double w) const { return (uint64_t)(w * kWeightUnit + 0.5); }
     __device__ uint64_t kept(float x, uint32_t index) const
     {
@@ -87,194 +172,717 @@ struct RowLimits {
     }
 };
 
-struct SampleShared {
-    unsigned long long mass[kBins];
-    uint32_t count[kBins];
-    uint64_t part[kSampleWaves];
-    uint64_t before, prefix;
-    uint32_t single, token;
+// A row's parameters.
+struct RowParams {
+    float temperature, top_p, min_p, u;
+    int32_t top_k;           // 0: all
+    __device__ RowParams(const SampleProblem &p, uint32_t r)
+    {
+        const u32x4 w = *(const Global<u32x4> *)((const Global<uint32_t> *)p.params + 4 * (uint64_t)r);
+        temperature = as_float(w[0]) > FLT_MAX ? FLT_MAX : as_float(w[0]);
+        top_k = max((int32_t)w[1], 0);
+        if ((uint32_t)top_k >= p.V) top_k = 0;
+        top_p = as_float(w[2]);
+        min_p = as_float(w[3]) > 0.0f ? fminf(as_float(w[3]), 1.0f) : 0.0f;
+        u = ((const Global<float> *)p.u)[r];
+    }
+    __device__ bool greedy() const { return !(temperature > 0.0f) || top_k == 1; }
+    __device__ bool limited() const { return top_k || top_p < 1.0f || min_p > 0.0f; }
+    __device__ bool wants_mass() const { return !greedy() && (top_p < 1.0f ? top_k == 0 : !limited()); }
+    // Weight with which top_p is reached, of a total.
+    __device__ uint64_t share(double total) const { return max((uint64_t)ceil(fmax((double)top_p, 0.0) * total), (uint64_t)1); }
+    // The kept weight in front of the token: u of NaN and below 0 is 0.
+    __device__ double before(double total) const { return fmin(fmax((double)u, 0.0), 1.0) * total; }
 };
 
-// Sum, or largest, of every thread's number.
-template <bool MAX>
-__device__ inline uint64_t block_u64(uint64_t v, SampleShared &s)
+// Bins of weight: numbered by the logit alone, so that those of different slices can be added.  Larger is earlier.
+struct BinScale {
+    float scale;             // 16 log2(e) / temperature
+    __device__ explicit BinScale(float temperature) : scale(16.0f * 1.4426950f / temperature) {}
+    __device__ bool usable() const { return scale > 1e-30f && scale < 1e30f; }
+    __device__ float raw(float x) const { return fminf(fmaxf(x * scale, -1e6f), 1e6f); }
+    __device__ int32_t of(float x) const { return (int32_t)floorf(raw(x)); }      // (all whole numbers of this size are floats)
+};
+
+constexpr uint32_t kSliceLoads = kSlice / 8 / kSliceThreads;      // units of a thread
+// The sum of eight weights, and each: as Weights::of, but what is below 2^-64 counts as that.
+struct SliceWeights {
+    double top, per, least;
+    __device__ SliceWeights(float t, float temperature) : top(t), per(1.4426950408889634 / (double)temperature), least(-64.0 / per) {}
+    __device__ double of(float x) const { return power_of_two(fmax((double)x - top, least), per); }
+};
+
+struct SliceShared {
+    f32x4 x[2 * kSliceLoads * kSliceThreads];      // a thread's j-th unit: four logits at 2 j kSliceThreads + its number, four kSliceThreads further
+    uint32_t keys[kSliceThreads], counts[kSliceWaves], firsts[kSliceWaves], down_to;
+    double masses[kSliceWaves];
+    unsigned long long bins[kMassBins];
+};
+
+__device__ inline void slice_row(const SampleProblem &p, uint32_t r, uint32_t slice, SliceShared &s)
 {
-    v = MAX ? wave_max_u64(v) : wave_sum_u64(v);
+    const LogitRow row(p, r);
+    const RowParams q(p, r);
+    const RowWork work(p, r);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), run = (work.units + kSliceWaves - 1) / kSliceWaves,
+                   base = slice * work.units + wave * run, end = min(min(base + run, (slice + 1) * work.units), row.units()), from = base + lane;
+    float mine = -INFINITY;
+    {
+        LogitRow::Raw raw[kSliceLoads];
+#pragma unroll
+        for (uint32_t j = 0; j < kSliceLoads; ++j)
+            if (from + 64 * j < end) raw[j] = row.raw(from + 64 * j);
+#pragma unroll
+        for (uint32_t j = 0; j < kSliceLoads; ++j) {
+            float x[8];
+            if (from + 64 * j < end) row.convert(raw[j], from + 64 * j, x);
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mine = fmaxf(mine, x[i]);
+            s.x[(2 * j) * kSliceThreads + threadIdx.x] = f32x4{x[0], x[1], x[2], x[3]};
+            s.x[(2 * j + 1) * kSliceThreads + threadIdx.x] = f32x4{x[4], x[5], x[6], x[7]};
+        }
+    }
+    s.keys[threadIdx.x] = key_of(mine);
+    const bool massed = q.wants_mass(), limited = q.limited() && !q.greedy();
+    const BinScale scale(q.temperature);
+    const bool binned = massed && q.top_p < 1.0f && scale.usable();
+    if (binned)
+        for (uint32_t i = threadIdx.x; i < kMassBins; i += kSliceThreads) s.bins[i] = 0;
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) s.part[threadIdx.x >> 6] = v;
+    // every wavefront has all of them
+    const u32x4 key0 = *(const u32x4 *)&s.keys[4 * lane], key1 = *(const u32x4 *)&s.keys[256 + 4 * lane];
+    const uint32_t key[8] = {key0[0], key0[1], key0[2], key0[3], key1[0], key1[1], key1[2], key1[3]};
+    static_assert(kSliceThreads == 512, "eight a lane");
+    uint32_t lane_key = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lane_key = max(lane_key, key[i]);
+    const float top = float_of(wave_largest(lane_key));
+    const bool listed = limited && top != -INFINITY;
+    if (listed && wave == 0) {
+        // The lists' threshold, which at least `want` of the threads' largest logits reach, and at most a quarter more than that where a few steps
+        // find such a one.  Each lane has eight of them: the smallest of the lanes' largest is reached by 64.
+        const uint32_t want = q.top_k ? min(min((uint32_t)q.top_k, 2 * (uint32_t)q.top_k / work.slices + 32), 128u) : 64u;
+        uint32_t down_to = want <= 64 ? ~wave_largest(~lane_key) : 0, above = key_of(top);
+#pragma unroll 1
+        for (int step = 0; step < 32 && above - down_to > 1; ++step) {
+            const uint32_t to = down_to + (above - down_to) / 2;
+            uint32_t reached = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) reached += __popcll(__ballot(key[i] >= to));
+            if (reached < want) above = to;
+            else {
+                down_to = to;
+                if (reached <= want + want / 4) break;
+            }
+        }
+        // nothing that min_p keeps lies below this (the margin is for the roundings of this line)
+        if (q.min_p > 0.0f) {
+            const float below = q.temperature * logf(q.min_p);
+            down_to = max(down_to, key_of(top + below - 1e-5f * (fabsf(top) + fabsf(below))));
+        }
+        if (lane == 0) s.down_to = max(down_to, key_of(-INFINITY) + 1);
+    }
+    if (limited) __syncthreads();
+    const float low = listed ? float_of(s.down_to) : INFINITY;
+    const bool has_top = __any(mine == top);
+    const int32_t top_bin = scale.of(top);
+    const SliceWeights weights(top, q.temperature);
+    Global<uint64_t> *list = work.list(slice, wave);
+    uint32_t first = ~0u, count = 0;
+    double mass = 0;
+#pragma unroll 1
+    for (uint32_t j = 0; j < kSliceLoads; ++j) {
+        const f32x4 a = s.x[2 * j * kSliceThreads + threadIdx.x], b = s.x[(2 * j + 1) * kSliceThreads + threadIdx.x];
+        const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        const uint32_t index = (from + 64 * j) * 8;
+        if (has_top) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) first = x[i] == top ? min(first, index + i) : first;
+        }
+        if (listed) {
+            uint32_t taken = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) taken |= (x[i] >= low ? 1u : 0u) << i;
+            if (__any(taken != 0)) {
+                const uint32_t up_to = count + wave_sum_scan((uint32_t)__popc(taken));
+                uint32_t to = up_to - __popc(taken);
+                count = lane_value(up_to, 63);
+                if (count <= kListed)
+                    while (taken) {
+                        const uint32_t i = __builtin_ctz(taken);
+                        taken &= taken - 1;
+                        list[to++] = place_of(s.x[(2 * j + i / 4) * kSliceThreads + threadIdx.x][i % 4], index + i);
+                    }
+            }
+        }
+        if (massed && top != -INFINITY) {
+#pragma unroll
+            for (int half = 0; half < 8; half += 4) {
+                double w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = top == INFINITY ? (x[half + i] == top ? 1.0 : 0.0) : weights.of(x[half + i]);
+                mass += (w[0] + w[1]) + (w[2] + w[3]);
+                if (binned) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t bin = (uint32_t)(top_bin - scale.of(x[half + i]));
+                        // w + 2^8 is w in units, rounded, in front of the bits of 2^8
+                        if (bin < kMassBins) atomicAdd(&s.bins[bin], (unsigned long long)(__builtin_bit_cast(uint64_t, w[i] + 256.0) - 0x4070000000000000ull));
+                    }
+                }
+            }
+        }
+    }
+    if (has_top) first = ~wave_largest(~first);
+    if (massed) mass = wave_total(mass);
+    if (lane == 0) {
+        s.counts[wave] = count;
+        s.firsts[wave] = first;
+        s.masses[wave] = mass;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        Slice out{};
+        uint32_t index = ~0u;
+#pragma unroll
+        for (uint32_t i = 0; i < kSliceWaves; ++i) {
+            index = min(index, s.firsts[i]);
+            out.mass += s.masses[i];
+            out.count[i] = s.counts[i];
+        }
+        out.first = top == -INFINITY ? 0 : place_of(top, index);
+        out.down_to = listed ? s.down_to : 0;
+        out.bin = top_bin;
+        out.binned = binned;
+        work.store(slice, out);
+    }
+    if (binned)
+        for (uint32_t i = threadIdx.x; i < kMassBins; i += kSliceThreads) work.bins(slice)[i] = s.bins[i];
+}
+
+template <typename Args>
+__global__ __launch_bounds__(kSliceThreads, 8) void slice_rows(Args a)
+{
+    __shared__ SliceShared s;
+    SampleProblem p;
+    const uint32_t t = find_owner(a.first, a.p, a.base + blockIdx.x, p), slices = slices_of(p.V);
+    slice_row(p, t / slices, t % slices, s);
+}
+
+// The code of this kernel runs once a row: what is not kept short is waited for line by line, so that loops are not unrolled and paths share their pieces.
+constexpr uint32_t kPieceSums = 32;      // of a wavefront: a piece of a row has at most 2^19 / 16 tokens
+struct ChooseShared {
+    unsigned long long mass[kBins];
+    uint32_t count[kBins];
+    uint64_t places[kMostListed];
+    uint64_t sums[kPieceSums * kSampleWaves];
+    uint64_t part[kSampleWaves];
+    double pieces[64];
+    uint64_t before, prefix;
+    uint32_t single, listed;
+    int32_t token;
+};
+
+// Which of up to 64 pieces of a row (lane i: their kept weights, of the largest) has the token, and the weight in front of it there.
+struct Piece { uint32_t at; double left; };
+__device__ inline Piece choose_piece(const RowParams &q, double mass)
+{
+    const double all = wave_sum_scan(mass), target = q.before(lane_value(all, 63));
+    // the first that passes the target, or the last that has any weight
+    const uint64_t past = __ballot(all > target && mass > 0.0), any = __ballot(mass > 0.0);
+    const uint32_t at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(any | 1);
+    return {at, target - (at ? lane_value(all, at - 1) : 0.0)};
+}
+
+// The token among logits from .. to of a row, `left` (of the largest weight) in front of it there; `first` if nothing there weighs half a unit.
+__device__ inline int32_t choose_in(const LogitRow &row, const RowLimits &l, uint32_t from, uint32_t to, double left, uint32_t first, ChooseShared &c)
+{
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();
+    uint32_t n = 0;
+#pragma unroll 1
+    for (uint32_t at = from; at < to; at += kSampleThreads, ++n) {
+        const uint32_t i = at + threadIdx.x;
+        const uint64_t sum = wave_total(i < to ? l.kept(row[i], i) : 0);
+        if (lane == 0) c.sums[n * kSampleWaves + wave] = sum;
+    }
+    if (threadIdx.x == 0) c.token = (int32_t)first;
+    __syncthreads();
+    if (wave != 0) {
+        __syncthreads();
+        return c.token;
+    }
+    // runs of sums: one wavefront finds whose token it is, and the token
+    n *= kSampleWaves;
+    constexpr uint32_t kEach = kPieceSums * kSampleWaves / 64;
+    uint64_t mine = 0;
+    for (uint32_t i = 0; i < kEach; ++i) mine += kEach * lane + i < n ? c.sums[kEach * lane + i] : 0;
+    const uint64_t scan = wave_sum_scan(mine), all = lane_value(scan, 63);
+    if (all != 0) {
+        // (the sums of pieces are rounded otherwise: the last token that weighs anything if none passes)
+        const uint64_t want = min((uint64_t)(fmax(left, 0.0) * kWeightUnit), all - 1);
+        const uint32_t owner = __builtin_ctzll(__ballot(scan > want));
+        uint64_t before = lane_value(scan - mine, owner);
+        uint32_t run = kEach * owner;
+        while (before + c.sums[run] <= want) before += c.sums[run++];
+        const uint32_t i = from + run * 64 + lane;
+        const uint64_t w = i < to ? l.kept(row[i], i) : 0;
+        const uint64_t past = __ballot(before + wave_sum_scan(w) > want);
+        if (lane == 0) c.token = (int32_t)(from + run * 64 + __builtin_ctzll(past));
+    }
+    __syncthreads();
+    return c.token;
+}
+
+// The token of a row by reading all of it, once what is kept of it is known (l.cut, l.min_p): sixteen runs.
+__device__ inline int32_t choose_by_runs(const LogitRow &row, const RowParams &q, const RowLimits &l, ChooseShared &c)
+{
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, run = (row.V + kSampleThreads - 1) / kSampleThreads * 64;
+    const uint32_t from = min(wave * run, row.V), to = min(from + run, row.V);
+    uint64_t sum = 0;
+#pragma unroll 2
+    for (uint32_t i = from + lane; i < to; i += 64) sum += l.kept(row[i], i);
+    sum = wave_total(sum);
+    __syncthreads();
+    if (lane == 0) c.part[wave] = sum;
+    __syncthreads();
+    const Piece piece = choose_piece(q, lane < kSampleWaves ? (double)c.part[lane] / kWeightUnit : 0.0);
+    return choose_in(row, l, piece.at * run, min(piece.at * run + run, row.V), piece.left, index_of(l.first), c);
+}
+
+__device__ inline uint64_t block_total(uint64_t v, ChooseShared &c)
+{
+    v = wave_total(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) c.part[threadIdx.x >> 6] = v;
     __syncthreads();
     uint64_t all = 0;
-#pragma unroll
-    for (uint32_t i = 0; i < kSampleWaves; ++i) all = MAX ? max(all, s.part[i]) : all + s.part[i];
+    for (uint32_t i = 0; i < kSampleWaves; ++i) all += c.part[i];
     return all;
 }
 
-// The place of the token with which the first ones of the order reach `target`, tokens or weight (WEIGHT), among those down to l.cut.
-template <bool BF16, bool WEIGHT>
-__device__ inline uint64_t reach(const LogitRow<BF16> &row, const RowLimits &l, uint64_t target, SampleShared &s)
+// The place of the token with which the first ones of the row's order reach `target`, tokens or weight, among those down to l.cut.
+__device__ inline uint64_t reach(const LogitRow &row, const RowLimits &l, bool by_weight, uint64_t target, ChooseShared &c)
 {
     uint64_t prefix = 0;                     // the bits known so far
     uint32_t left = kPlaceBits;
     for (;;) {
         const uint32_t bits = min(left, 11u), rest = left - bits;
         for (uint32_t i = threadIdx.x; i < kBins; i += kSampleThreads) {
-            s.mass[i] = 0;
-            s.count[i] = 0;
+            c.mass[i] = 0;
+            c.count[i] = 0;
         }
         __syncthreads();
-        for (uint32_t unit = threadIdx.x; unit < row.units(); unit += kSampleThreads) {
-            float x[8];
-            row.load(unit, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint64_t place = place_of(x[i], unit * 8 + i);
-                if (place < l.cut || x[i] == -INFINITY || (left < kPlaceBits && place >> left != prefix)) continue;
-                const uint32_t bin = kBins - 1 - ((uint32_t)(place >> rest) & ((1u << bits) - 1));
-                atomicAdd(&s.count[bin], 1u);
-                if (WEIGHT) atomicAdd(&s.mass[bin], (unsigned long long)l.units(l.weight(x[i])));
-            }
+#pragma unroll 1
+        for (uint32_t i = threadIdx.x; i < row.V; i += kSampleThreads) {
+            const float x = row[i];
+            const uint64_t place = place_of(x, i);
+            if (x == -INFINITY || place < l.cut || (left < kPlaceBits && place >> left != prefix)) continue;
+            const uint32_t bin = kBins - 1 - ((uint32_t)(place >> rest) & ((1u << bits) - 1));
+            atomicAdd(&c.count[bin], 1u);
+            if (by_weight) atomicAdd(&c.mass[bin], (unsigned long long)l.units(l.weight(x)));
         }
         __syncthreads();
         // two bins a thread, the earliest tokens in front
         const uint32_t b = 2 * threadIdx.x;
-        const uint64_t n0 = WEIGHT ? s.mass[b] : s.count[b], n1 = WEIGHT ? s.mass[b + 1] : s.count[b + 1];
-        uint64_t total;
-        uint64_t before = wave_excl_scan_u64(n0 + n1, &total);
-        if ((threadIdx.x & 63) == 0) s.part[threadIdx.x >> 6] = total;
+        const uint64_t n0 = by_weight ? c.mass[b] : c.count[b], n1 = by_weight ? c.mass[b + 1] : c.count[b + 1];
+        const uint64_t up_to = wave_sum_scan(n0 + n1);
+        uint64_t before = up_to - (n0 + n1);
+        if ((threadIdx.x & 63) == 63) c.part[threadIdx.x >> 6] = up_to;
         __syncthreads();
-        for (uint32_t i = 0; i < threadIdx.x >> 6; ++i) before += s.part[i];
+        for (uint32_t i = 0; i < threadIdx.x >> 6; ++i) before += c.part[i];
         const bool one = before < target && target <= before + n0, two = before + n0 < target && target <= before + n0 + n1;
         if (one || two) {
             const uint32_t bin = b + two;
-            s.before = before + (two ? n0 : 0);
-            s.prefix = (left < kPlaceBits ? prefix << bits : 0) | ((kBins - 1 - bin) & ((1u << bits) - 1));
-            s.single = s.count[bin] == 1;
+            c.before = before + (two ? n0 : 0);
+            c.prefix = (left < kPlaceBits ? prefix << bits : 0) | ((kBins - 1 - bin) & ((1u << bits) - 1));
+            c.single = c.count[bin] == 1;
         }
         __syncthreads();
-        prefix = s.prefix;
-        target -= s.before;
+        prefix = c.prefix;
+        target -= c.before;
         left = rest;
-        const bool done = s.single || left == 0;
+        const bool done = c.single || left == 0;
         __syncthreads();
         if (done) return prefix << left;
     }
 }
 
-template <bool BF16>
-__device__ inline int32_t sample_row(const SampleProblem &p, uint32_t r, SampleShared &s)
+// The token of a row by reading it as often as it takes; l.cut is 0.
+__device__ inline int32_t choose_anywhere(const LogitRow &row, const RowParams &q, RowLimits &l, ChooseShared &c)
 {
-    const LogitRow<BF16> row{(const Global<char> *)p.logits + (uint64_t)r * p.ld * (BF16 ? 2 : 4), p.V};
-    const u32x4 params = *(const Global<u32x4> *)((const Global<uint32_t> *)p.params + 4 * (uint64_t)r);
-    const float temperature = as_float(params[0]), top_p = as_float(params[2]), min_p = as_float(params[3]), u = ((const Global<float> *)p.u)[r];
-    const int32_t top_k = (int32_t)params[1];
-    uint64_t first = 0;
-    for (uint32_t unit = threadIdx.x; unit < row.units(); unit += kSampleThreads) {
-        float x[8];
-        row.load(unit, x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (x[i] != -INFINITY) first = max(first, place_of(x[i], unit * 8 + i));
-    }
-    first = block_u64<true>(first, s);
-    if (first == 0) return -1;
-    if (!(temperature > 0.0f) || top_k == 1) return (int32_t)index_of(first);
-    RowLimits l{logit_of(first), 1.0 / (double)temperature, first, 0, min_p > 0.0f ? fmin(1.0, (double)min_p) : 0.0};
-    const auto sum_kept = [&](bool limits) {
-        uint64_t sum = 0;
-        for (uint32_t unit = threadIdx.x; unit < row.units(); unit += kSampleThreads) {
-            float x[8];
-            row.load(unit, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                sum += limits ? l.kept(x[i], unit * 8 + i) : place_of(x[i], unit * 8 + i) >= l.cut && x[i] != -INFINITY ? l.units(l.weight(x[i])) : 0;
-        }
-        return block_u64<false>(sum, s);
-    };
-    if (top_k > 0 && (uint32_t)top_k < p.V) {
+    __syncthreads();
+    if (q.top_k) {
         // logits of minus infinity have no place: fewer may be left
         uint64_t count = 0;
-        for (uint32_t unit = threadIdx.x; unit < row.units(); unit += kSampleThreads) {
-            float x[8];
-            row.load(unit, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) count += x[i] != -INFINITY;
+        for (uint32_t i = threadIdx.x; i < row.V; i += kSampleThreads) count += row[i] != -INFINITY;
+        count = block_total(count, c);
+        if ((uint32_t)q.top_k < count) l.cut = reach(row, l, false, (uint32_t)q.top_k, c);
+    }
+    if (q.top_p < 1.0f) {
+        uint64_t total = 0;
+        for (uint32_t i = threadIdx.x; i < row.V; i += kSampleThreads) {
+            const float x = row[i];
+            total += x != -INFINITY && place_of(x, i) >= l.cut ? l.units(l.weight(x)) : 0;
         }
-        count = block_u64<false>(count, s);
-        if ((uint32_t)top_k < count) l.cut = reach<BF16, false>(row, l, (uint32_t)top_k, s);
+        total = block_total(total, c);
+        l.cut = max(l.cut, reach(row, l, true, min(q.share((double)total), total), c));
     }
-    if (top_p < 1.0f) {
-        const uint64_t total = sum_kept(false);
-        const double want = ceil(fmax((double)top_p, 0.0) * (double)total);
-        l.cut = max(l.cut, reach<BF16, true>(row, l, min(max((uint64_t)want, (uint64_t)1), total), s));
+    return choose_by_runs(row, q, l, c);
+}
+
+// The lists of a row's slices, one behind the other, so in order of index; how many, more than kMostListed if they do not fit.
+__device__ inline uint32_t gather_lists(const RowWork &work, const Slice &mine, ChooseShared &c)
+{
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t most = 0, own = 0;
+#pragma unroll
+    for (uint32_t v = 0; v < kSliceWaves; ++v) {
+        most = max(most, mine.count[v]);
+        own = min(own + mine.count[v], kMostListed + 1);
     }
-    // in order of index: a wavefront has a run of units
-    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, run = (row.units() + kSampleWaves - 1) / kSampleWaves;
-    const uint32_t from = wave * run, to = min(from + run, row.units());
+    const uint32_t scan = wave_sum_scan(own), all = lane_value(scan, 63);
+    if (__any(most > kListed) || all > kMostListed) return kMostListed + 1;
+    // where each list goes
+    if (wave == 0 && lane < work.slices) {
+        uint32_t to = scan - own;
+#pragma unroll
+        for (uint32_t v = 0; v < kSliceWaves; ++v) {
+            c.count[lane * kSliceWaves + v] = to;
+            to += mine.count[v];
+            c.count[1024 + lane * kSliceWaves + v] = to;
+        }
+    }
+    __syncthreads();
+    static_assert(kListed == 64 && kSliceWaves * 64 <= 1024, "one a lane");
+    const Global<uint64_t> *lists = work.list(0, 0);
+#pragma unroll 4
+    for (uint32_t i = wave; i < work.slices * kSliceWaves; i += kSampleWaves) {
+        const uint32_t to = c.count[i] + lane;
+        if (to < c.count[1024 + i]) c.places[to] = lists[i * kListed + lane];
+    }
+    __syncthreads();
+    return all;
+}
+
+// What follows is one wavefront's: the lists are short, and barriers of sixteen wavefronts would take longer than what lies between them.
+
+// As reach(), among places[0 .. count); 256 bins at a time of the range that the places take.
+__device__ inline uint64_t reach_listed(const uint64_t *places, uint32_t count, const RowLimits &l, bool by_weight, uint64_t target, ChooseShared &c)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    uint64_t from = ~0ull, span = 0;             // the token is among from .. from + span - 1
+    for (uint32_t i = lane; i < count; i += 64) {
+        from = min(from, places[i]);
+        span = max(span, places[i]);
+    }
+    from = ~wave_largest(~from);
+    span = wave_largest(span) - from + 1;
+#pragma unroll 1
+    for (;;) {
+        const uint32_t bits = 64 - __builtin_clzll(span - 1 | 1), shift = bits > 8 ? bits - 8 : 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            c.count[4 * lane + i] = 0;
+            c.mass[4 * lane + i] = 0;
+        }
+        wave_sync();
+#pragma unroll 1
+        for (uint32_t i = lane; i < count; i += 64) {
+            const uint64_t place = places[i], off = place - from;
+            if (place < from || off >= span) continue;
+            const uint32_t bin = 255 - (uint32_t)(off >> shift);
+            atomicAdd(&c.count[bin], 1u);
+            if (by_weight) atomicAdd(&c.mass[bin], (unsigned long long)l.units(l.weight(logit_of(place))));
+        }
+        wave_sync();
+        // four bins a lane, the earliest tokens in front
+        uint64_t n[4], sum = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) sum += n[i] = by_weight ? c.mass[4 * lane + i] : c.count[4 * lane + i];
+        const uint64_t scan = wave_sum_scan(sum);
+        uint64_t before = scan - sum;
+        const uint32_t owner = __builtin_ctzll(__ballot(scan >= target) | 1ull << 63);
+        uint32_t bin = 4 * lane;
+        uint64_t in_front = before;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            if (before < target && target <= before + n[i]) {
+                bin = 4 * lane + i;
+                in_front = before;
+            }
+            before += n[i];
+        }
+        bin = lane_value(bin, owner);
+        target -= lane_value(in_front, owner);
+        from += (uint64_t)(255 - bin) << shift;
+        span = 1ull << shift;
+        const bool single = c.count[bin] == 1;
+        wave_sync();
+        if (shift == 0 || single) return from;
+    }
+}
+
+// Leaves of places[0 .. count) those down to `cut`, in order; how many.
+__device__ inline uint32_t keep_from(uint64_t *places, uint32_t count, uint64_t cut)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t n = 0;
+#pragma unroll 1
+    for (uint32_t at = 0; at < count; at += 64) {
+        const uint64_t place = at + lane < count ? places[at + lane] : 0;
+        const bool kept = at + lane < count && place >= cut;
+        const uint64_t all = __ballot(kept);
+        wave_sync();
+        if (kept) places[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] = place;
+        n += __popcll(all);
+    }
+    wave_sync();
+    return n;
+}
+
+__device__ inline uint64_t listed_weight(const uint64_t *places, uint32_t count, const RowLimits &l)
+{
     uint64_t sum = 0;
-    for (uint32_t unit = from + lane; unit < to; unit += 64) {
-        float x[8];
-        row.load(unit, x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += l.kept(x[i], unit * 8 + i);
+#pragma unroll 1
+    for (uint32_t i = threadIdx.x & 63; i < count; i += 64) sum += l.kept(logit_of(places[i]), index_of(places[i]));
+    return wave_total(sum);
+}
+
+// The token of a row whose lists have what its limits may keep: known down to `down_to` (the upper bits of a place).  total: the row's weight, if it is known.  -1 if the lists
+// do not tell.
+__device__ inline int32_t choose_listed(uint32_t count, const RowParams &q, RowLimits l, uint32_t down_to, double total, ChooseShared &c)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    const double min_p = l.min_p;
+    l.min_p = 0;             // (for the sums)
+    // everything there is is known, or everything that min_p keeps
+    const bool everything = down_to <= key_of(-INFINITY) + 1;
+    bool known = everything || (min_p > 0.0 && l.weight(float_of(down_to)) < min_p);
+    uint64_t cut = (uint64_t)down_to << 20;
+    // by the threshold, by top_k, by top_p
+#pragma unroll 1
+    for (int limit = 0;; ++limit) {
+        count = keep_from(c.places, count, cut);
+        bool by_weight = false;
+        uint64_t target;
+        if (limit == 0 && q.top_k) {
+            if (count >= (uint32_t)q.top_k) known = true;
+            else if (!everything && q.top_p < 1.0f) return -1;         // the sum of what top_k keeps is not known
+            if (count <= (uint32_t)q.top_k) continue;
+            target = (uint32_t)q.top_k;
+        } else if (limit <= 1 && q.top_p < 1.0f) {
+            const uint64_t weight = listed_weight(c.places, count, l);
+            const bool all = everything || q.top_k;      // these are all that share the weight
+            target = all ? min(q.share((double)weight), weight) : q.share(total);
+            by_weight = true;
+            limit = 1;
+            if (target > weight) break;
+            known = true;
+        } else break;
+        cut = reach_listed(c.places, count, l, by_weight, target, c);
     }
-    sum = wave_sum_u64(sum);
-    __syncthreads();
-    if (lane == 0) s.part[wave] = sum;
-    __syncthreads();
-    uint64_t all = 0, before = 0;
-    for (uint32_t i = 0; i < kSampleWaves; ++i) {
-        if (i == wave) before = all;
-        all += s.part[i];
+    if (!known) return -1;
+    l.min_p = min_p;
+    const uint64_t all = listed_weight(c.places, count, l), want = min((uint64_t)q.before((double)all), all - 1);      // (the product may be rounded up)
+    uint64_t before = 0;
+#pragma unroll 1
+    for (uint32_t at = 0;; at += 64) {
+        const uint64_t w = at + lane < count ? l.kept(logit_of(c.places[at + lane]), index_of(c.places[at + lane])) : 0, scan = before + wave_sum_scan(w);
+        const uint64_t past = __ballot(scan > want);
+        if (past) return (int32_t)index_of(c.places[at + __builtin_ctzll(past)]);
+        before = lane_value(scan, 63);
     }
-    // u of NaN and below 0 is 0; the product is below the sum also where it is rounded up
-    const uint64_t target = min((uint64_t)(fmin(fmax((double)u, 0.0), 1.0) * (double)all), all - 1);
-    if (before <= target && target < before + sum) {
-        for (uint32_t step = from; step < to; step += 64) {
-            uint64_t w[8], mine = 0;
+}
+
+// The bin in which the row's weight reaches `share` units (lane i: slice i), by all slices' bins, and how much of it that takes; false if it is none of theirs.
+// front: lane i gets slice i's weight in front of it.
+struct LastBin { int32_t bin; double want, front; };
+__device__ inline bool find_bin(const RowWork &work, const RowLimits &l, const Slice &mine, int32_t top_bin, double share, LastBin &last, ChooseShared &c)
+{
+    static_assert(kMassBins <= kSampleThreads && kMassBins % 64 == 0, "a bin a thread");
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const double factor = mine.first ? l.weight(logit_of(mine.first)) : 0.0;
+    if (__any(lane < work.slices && mine.first && !mine.binned)) return false;
+    double sum = 0;
+    if (threadIdx.x < kMassBins) {
+#pragma unroll 1
+        for (uint32_t i0 = 0; i0 < work.slices; i0 += 8) {
+            uint64_t v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = 0;
-            const uint32_t unit = step + lane;
-            if (unit < to) {
-                float x[8];
-                row.load(unit, x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) mine += w[i] = l.kept(x[i], unit * 8 + i);
+            for (uint32_t k = 0; k < 8; ++k) {
+                const uint32_t i = min(i0 + k, work.slices - 1), bin = threadIdx.x - (uint32_t)(top_bin - lane_value(mine.bin, i));
+                v[k] = 0;
+                if (i0 + k < work.slices && lane_value(factor, i) > 0.0 && bin < kMassBins) v[k] = work.bins(i)[bin];
             }
-            uint64_t total, at = before + wave_excl_scan_u64(mine, &total);
-            if (at <= target && target < at + mine) {
-                uint32_t token = unit * 8;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (at <= target && target < at + w[i]) token = unit * 8 + i;
-                    at += w[i];
-                }
-                s.token = token;
+            for (uint32_t k = 0; k < 8; ++k) sum = fma((double)v[k], lane_value(factor, min(i0 + k, work.slices - 1)), sum);
+        }
+    }
+    double *part = (double *)c.part;
+    const double up_to = wave_sum_scan(sum);
+    __syncthreads();
+    if (threadIdx.x == 0) c.single = 0;
+    if (lane == 63) part[wave] = up_to;
+    __syncthreads();
+    double before = 0;
+    for (uint32_t i = 0; i < wave; ++i) before += part[i];
+    // the first bin that reaches it: sums rounded differently may leave none or two at a border of wavefronts, of which none is taken
+    if (threadIdx.x < kMassBins && before + (up_to - sum) < share && share <= before + up_to && atomicAdd(&c.single, 1u) == 0) {
+        c.before = __builtin_bit_cast(uint64_t, share - (before + (up_to - sum)));
+        c.prefix = (uint64_t)(int64_t)(top_bin - (int32_t)threadIdx.x);
+    }
+    __syncthreads();
+    last.want = __builtin_bit_cast(double, c.before);
+    last.bin = (int32_t)c.prefix;
+    if (c.single != 1) return false;
+#pragma unroll 1
+    for (uint32_t i = wave; i < work.slices; i += kSampleWaves) {
+        const int32_t bins = lane_value(mine.bin, i) - last.bin;       // of this slice in front of the last
+        const double f = lane_value(factor, i);
+        uint64_t v = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kMassBins / 64; ++k)
+            if (f > 0.0 && (int32_t)(lane + 64 * k) < bins) v += work.bins(i)[lane + 64 * k];
+        const uint64_t all = wave_total(v);
+        if (lane == 0) c.pieces[i] = (double)all / kWeightUnit * f;
+    }
+    __syncthreads();
+    last.front = lane < work.slices ? c.pieces[lane] : 0.0;
+    return true;
+}
+
+// Finds the last kept place (l.cut) in the bin in which top_p ends: reads the row for the bin's tokens; false if they are too many.
+__device__ inline bool cut_in_bin(const LogitRow &row, const RowParams &q, RowLimits &l, const LastBin &last, ChooseShared &c)
+{
+    const uint32_t lane = threadIdx.x & 63, units = row.units();
+    const BinScale scale(q.temperature);
+    const float from = (float)last.bin, to = (float)(last.bin + 1);
+    if (threadIdx.x == 0) c.listed = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (uint32_t unit = threadIdx.x; unit < units; unit += 2 * kSampleThreads) {
+        LogitRow::Raw raw[2];
+        raw[0] = row.raw(unit);
+        if (unit + kSampleThreads < units) raw[1] = row.raw(unit + kSampleThreads);
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+            if (unit + k * kSampleThreads >= units) break;
+            float x[8];
+            row.convert(raw[k], unit + k * kSampleThreads, x);
+            uint32_t marked = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float y = scale.raw(x[i]);
+                marked |= (y >= from && y < to && x[i] != -INFINITY ? 1u : 0u) << i;
             }
-            before += total;
-            if (before > target) break;
+            while (marked) {
+                const uint32_t i = __builtin_ctz(marked), index = (unit + k * kSampleThreads) * 8 + i, slot = atomicAdd(&c.listed, 1u);
+                marked &= marked - 1;
+                if (slot < kMostListed) c.places[slot] = place_of(row[index], index);
+            }
         }
     }
     __syncthreads();
-    return (int32_t)s.token;
+    const uint32_t count = c.listed;
+    if (count > kMostListed) return false;
+    if (threadIdx.x < 64) {
+        RowLimits all = l;
+        all.min_p = 0;
+        const uint64_t weight = listed_weight(c.places, count, all);
+        if (weight != 0) {
+            const uint64_t cut = reach_listed(c.places, count, l, true, min(max((uint64_t)ceil(last.want), (uint64_t)1), weight), c);
+            if (lane == 0) c.prefix = cut;
+        }
+        if (lane == 0) c.single = weight != 0;
+    }
+    __syncthreads();
+    l.cut = c.prefix;
+    return c.single != 0;
+}
+
+__device__ inline int32_t choose_row(const SampleProblem &p, uint32_t r, ChooseShared &c)
+{
+    const LogitRow row(p, r);
+    const uint32_t lane = threadIdx.x & 63;
+    const RowWork work(p, r);
+    // lane i of every wavefront has slice i
+    Slice mine{};
+    if (lane < work.slices) mine = work.load(lane);
+    const RowParams q(p, r);
+    const uint64_t first = wave_largest(mine.first);
+    if (first == 0) return -1;
+    if (q.greedy()) return (int32_t)index_of(first);
+    RowLimits l(first, q.temperature, q.min_p);
+    double mass = mine.first && q.wants_mass() ? mine.mass * l.weight(logit_of(mine.first)) : 0.0;
+    if (q.limited()) {
+        const double total = wave_total(mass) * kWeightUnit;
+        const uint32_t count = gather_lists(work, mine, c);
+        if (count <= kMostListed) {
+            const uint32_t down_to = wave_largest(lane < work.slices && mine.first ? mine.down_to : 0);
+            if (threadIdx.x < 64) {
+                const int32_t token = choose_listed(count, q, l, down_to, total, c);
+                if (lane == 0) c.token = token;
+            }
+            __syncthreads();
+            const int32_t token = c.token;
+            __syncthreads();
+            if (token >= 0) return token;
+        }
+        LastBin last;
+        const bool by_bin = !q.top_k && q.top_p < 1.0f && find_bin(work, l, mine, BinScale(q.temperature).of(l.top), (double)q.share(total), last, c) && cut_in_bin(row, q, l, last, c);
+        if (!by_bin) {
+            l.cut = 0;
+            if (q.top_k || q.top_p < 1.0f) return choose_anywhere(row, q, l, c);
+        }
+        if (q.min_p > 0.0f) return choose_by_runs(row, q, l, c);
+        // what is kept of the bin goes to the slices; the histogram's place holds their sums
+        __syncthreads();
+        if (threadIdx.x < 64) c.mass[threadIdx.x] = 0;
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < c.listed; j += kSampleThreads) {
+            const uint32_t index = index_of(c.places[j]);
+            const uint64_t w = l.kept(logit_of(c.places[j]), index);
+            if (w) atomicAdd(&c.mass[index / 8 / work.units], (unsigned long long)w);
+        }
+        __syncthreads();
+        mass = last.front + (double)c.mass[lane] / kWeightUnit;
+    }
+    const Piece piece = choose_piece(q, mass);
+    const uint32_t from = piece.at * work.units * 8;
+    return choose_in(row, l, from, min(from + work.units * 8, row.V), piece.left, index_of(lane_value(mine.first, piece.at)), c);
 }
 
 template <typename Args>
-__global__ __launch_bounds__(kSampleThreads) void sample_rows(Args a)
+__global__ __launch_bounds__(kSampleThreads) void choose_rows(Args a)
 {
-    __shared__ SampleShared s;
+    __shared__ ChooseShared s;
     SampleProblem p;
     const uint32_t r = find_owner(a.first, a.p, a.base + blockIdx.x, p);
-    const int32_t token = p.bf16 ? sample_row<true>(p, r, s) : sample_row<false>(p, r, s);
+    const int32_t token = choose_row(p, r, s);
     if (threadIdx.x == 0) ((Global<int32_t> *)p.tokens)[r] = token;
 }
 
-uint64_t sample_work_bytes(uint32_t M, uint32_t) { return 16ull * M; }
+uint64_t sample_work_bytes(uint32_t M, uint32_t V) { return M * RowWork::size(V); }
+
+namespace {
+
+template <uint32_t NP>
+hipError_t launch_sampling(const SampleProblem *p, uint32_t n, hipStream_t stream, uint64_t *launches)
+{
+    hipError_t e = launch_answer_of<SampleProblem, NP>(slice_rows, kSliceThreads, p, n, stream, launches, [](const SampleProblem &q) { return (uint64_t)q.M * slices_of(q.V); });
+    if (e == hipSuccess) e = launch_answer_of<SampleProblem, NP>(choose_rows, kSampleThreads, p, n, stream, launches, [](const SampleProblem &q) { return (uint64_t)q.M; });
+    return e;
+}
+
+}  // namespace
 
 hipError_t launch_sample(const SampleProblem *p, uint32_t n, hipStream_t stream, uint64_t *launches)
 {
-    const auto rows = [](const SampleProblem &q) { return (uint64_t)q.M; };
-    if (n <= kAnswerFew) return launch_answer_of<SampleProblem, kAnswerFew>(sample_rows, kSampleThreads, p, n, stream, launches, rows);
-    return launch_answer_of<SampleProblem, kAnswerProblems>(sample_rows, kSampleThreads, p, n, stream, launches, rows);
+    return n <= kAnswerFew ? launch_sampling<kAnswerFew>(p, n, stream, launches) : launch_sampling<kAnswerProblems>(p, n, stream, launches);
 }
 
 }  // namespace salus
