@@ -34,10 +34,10 @@ struct AttentionProblem {
     float scale;             // times log2(e)
     uint32_t part;           // keys of a part, a multiple of 128
     uint32_t parts;          // of a row at most
-    uint32_t pad;
+    uint32_t columns;        // of a tile
 };
-struct AttentionParts { uint32_t part, parts; };
-AttentionParts attention_parts(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len);
+struct AttentionParts { uint32_t columns, part, parts; };
+AttentionParts attention_parts(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len, uint32_t window);
 uint64_t attention_work_floats(uint32_t M, uint32_t Hq, uint32_t D, const AttentionParts &);
 hipError_t launch_attention(const AttentionProblem *p, uint32_t n, hipStream_t stream, uint64_t *launches);
 
@@ -86,37 +86,32 @@ inline hipError_t launch_answer_of(void (*kernel)(AnswerArgs<P, NP>), int thread
 struct SequenceTile {
     uint32_t s, row, n;      // the sequence, its first row, its rows
     uint32_t tile;           // number of the tile among those of the sequence
+    int32_t length;          // its tokens
 };
 
 // Tiles are numbered so that none has to be counted: sequence s begins at tile base(start of s, s), which leaves it as many as it can need, and
-// some that stay empty.  Sixty-four sequences are looked at at once, so that the search is one trip to memory for up to 64 of them, two for 4096.
+// some that stay empty.  Sixty-four sequences are looked at at once, their beginnings, ends and lengths, so that the search is one trip to memory for up to 64
+// of them, two for 4096.  length: at most `most`.
 template <typename Base>
-__device__ inline bool find_sequence(const Sequences &q, uint32_t t, Base base, SequenceTile &out)
+__device__ inline bool find_sequence(const Sequences &q, uint32_t t, Base base, uint32_t most, SequenceTile &out)
 {
     const uint32_t lane = threadIdx.x & 63;
-    const Global<int32_t> *starts = (const Global<int32_t> *)q.starts;
-    const auto start = [&](uint32_t s) { return (uint32_t)min(max(starts[s], 0), (int32_t)q.M); };
+    const Global<int32_t> *starts = (const Global<int32_t> *)q.starts, *lens = (const Global<int32_t> *)q.lens;
+    const auto row = [&](int32_t v) { return (uint32_t)min(max(v, 0), (int32_t)q.M); };
     uint32_t low = 0, span = q.n_seqs;
     for (;;) {
-        const uint32_t step = (span + 63) / 64, s = low + lane * step;
-        const bool mine = lane * step < span;
-        const uint64_t before = __ballot(mine && base(start(mine ? s : low), mine ? s : low) <= t);
+        const uint32_t step = (span + 63) / 64, s = min(low + lane * step, q.n_seqs - 1);
+        const uint32_t start = row(starts[s]), end = row(starts[s + 1]), length = (uint32_t)min(max(lens[s], 0), (int32_t)most);
+        const uint64_t before = __ballot(lane * step < span && base(start, s) <= t);
         if (before == 0) return false;
         const uint32_t at = 63 - __builtin_clzll(before);
         low += at * step;
         span = min(step, span - at * step);
-        if (span <= 1) break;
+        if (span > 1) continue;
+        const uint32_t first = lane_value(start, at), behind = lane_value(end, at);
+        out = {low, first, behind > first ? behind - first : 0, t - base(first, low), (int32_t)lane_value(length, at)};
+        return true;
     }
-    low = __builtin_amdgcn_readfirstlane(low);
-    const uint32_t first = __builtin_amdgcn_readfirstlane(start(low)), end = __builtin_amdgcn_readfirstlane(start(low + 1));
-    out = {low, first, end > first ? end - first : 0, t - base(first, low)};
-    return true;
-}
-
-// Tokens of sequence s, at most `most`.
-__device__ inline int32_t length_of(const Sequences &q, uint32_t s, uint32_t most)
-{
-    return __builtin_amdgcn_readfirstlane(min(max(((const Global<int32_t> *)q.lens)[s], 0), (int32_t)most));
 }
 
 }  // namespace salus

@@ -96,9 +96,9 @@ int32_t attention(salus_pool_t *pool, const salus_attention_desc *descs, uint32_
         if (persist.outside()) return kCache;
         if (lane.outside()) return kLane;
         if (lane.overlap()) return kOverlap;
-        const AttentionParts parts = attention_parts(d.M, d.n_seqs, d.Hq, d.Hkv, d.D, d.max_len);
+        const AttentionParts parts = attention_parts(d.M, d.n_seqs, d.Hq, d.Hkv, d.D, d.max_len, d.window);
         problems.push_back({seq, at.lane + d.q_off, at.persist + d.k_off, at.persist + d.v_off, at.lane + d.y_off,
-                            work ? (float *)(at.lane + d.work_off) : nullptr, d.max_len, d.window, d.scale * 1.4426950408889634f, parts.part, parts.parts, 0});
+                            work ? (float *)(at.lane + d.work_off) : nullptr, d.max_len, d.window, d.scale * 1.4426950408889634f, parts.part, parts.parts, parts.columns});
         return nullptr;
     });
     if (rc) return rc;
@@ -168,7 +168,7 @@ int32_t salus_grouped_append(salus_pool_t *pool, const salus_append_desc *descs,
 uint64_t salus_attention_work_bytes(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len)
 {
     if (!heads_ok(Hq, Hkv, D) || !seqs_ok(M, n_seqs, Hq, Hkv) || max_len == 0 || max_len >= 1u << 30) return 0;
-    return up256(4 * attention_work_floats(M, Hq, D, attention_parts(M, n_seqs, Hq, Hkv, D, max_len)));
+    return up256(4 * attention_work_floats(M, Hq, D, attention_parts(M, n_seqs, Hq, Hkv, D, max_len, 0)));
 }
 
 int32_t salus_grouped_attention(salus_pool_t *pool, const salus_attention_desc *descs, uint32_t n, void *stream)

@@ -11,16 +11,14 @@ namespace salus {
 
 constexpr uint32_t kKeys = 32;      // of a tile
 
-// Tiles of COLUMNS columns of a sequence: G query heads share a key head.
-template <uint32_t COLUMNS>
+// Tiles of `columns` columns of a sequence: G query heads share a key head.
 struct ColumnBase {
-    uint32_t G;
-    __host__ __device__ uint32_t operator()(uint32_t start, uint32_t s) const { return start * G / COLUMNS + s; }
+    uint32_t G, columns;
+    __host__ __device__ uint32_t operator()(uint32_t start, uint32_t s) const { return start * G / columns + s; }
 };
-template <uint32_t COLUMNS>
 inline uint64_t column_tiles(const AttentionProblem &q)
 {
-    return (uint64_t)ColumnBase<COLUMNS>{q.seq.Hq / q.seq.Hkv}(q.seq.M, q.seq.n_seqs) * q.seq.Hkv;
+    return (uint64_t)ColumnBase{q.seq.Hq / q.seq.Hkv, q.columns}(q.seq.M, q.seq.n_seqs) * q.seq.Hkv;
 }
 
 // A window, cut so that positions and windows can be subtracted.
@@ -36,22 +34,23 @@ struct ColumnTile {
     uint32_t part, parts;       // this workgroup's part of the keys, parts that are not empty
 };
 
-// COLUMNS: of a tile.  part: which of p.parts.
-template <uint32_t COLUMNS>
+// part: which of p.parts.  LAST_FIRST: a sequence's tiles from the last, which sees most, to the first.
+template <bool LAST_FIRST>
 __device__ inline bool find_columns(const AttentionProblem &p, uint32_t t, uint32_t part, ColumnTile &c)
 {
     const uint32_t G = p.seq.Hq / p.seq.Hkv;
     c.part = part;
     c.head = t % p.seq.Hkv;
     SequenceTile at;
-    if (!find_sequence(p.seq, t / p.seq.Hkv, ColumnBase<COLUMNS>{G}, at)) return false;
+    if (!find_sequence(p.seq, t / p.seq.Hkv, ColumnBase{G, p.columns}, p.max_len, at)) return false;
     c.s = at.s;
     c.row = at.row;
     c.n = at.n;
-    c.first = at.tile * COLUMNS;
-    if (c.first >= c.n * G) return false;
-    c.end = min(c.first + COLUMNS, c.n * G);
-    c.position = length_of(p.seq, at.s, p.max_len) - (int32_t)c.n;
+    const uint32_t tiles = (c.n * G + p.columns - 1) / p.columns;
+    if (at.tile >= tiles) return false;
+    c.first = (LAST_FIRST ? tiles - 1 - at.tile : at.tile) * p.columns;
+    c.end = min(c.first + p.columns, c.n * G);
+    c.position = at.length - (int32_t)c.n;
     c.key_end = max(c.position + (int32_t)((c.end - 1) / G) + 1, 0);
     c.key = p.window ? max(c.position + (int32_t)(c.first / G) - window_of(p) + 1, 0) & ~31 : 0;
     c.parts = c.key_end > c.key ? ((uint32_t)(c.key_end - c.key) + p.part - 1) / p.part : 0;

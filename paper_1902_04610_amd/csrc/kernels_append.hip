@@ -69,10 +69,10 @@ __global__ __launch_bounds__(kAppendThreads) void append_rows(Args a)
     AppendProblem p;
     const uint32_t t = find_owner(a.first, a.p, a.base + blockIdx.x, p);
     SequenceTile at;
-    if (!find_sequence(p.seq, t, append_base, at)) return;
-    const Sequences &s = p.seq;
     // a sequence may be longer than what max_pages hold: its tokens there have no page
-    const int32_t position = length_of(s, at.s, 0x7fffff00) - (int32_t)at.n;          // of the sequence's first new row
+    if (!find_sequence(p.seq, t, append_base, 0x7fffff00, at)) return;
+    const Sequences &s = p.seq;
+    const int32_t position = at.length - (int32_t)at.n;          // of the sequence's first new row
     const int32_t group = (position & ~7) + 8 * (int32_t)at.tile;                     // first token of the eight
     const int32_t from = max(group, position), to = min(group + 8, position + (int32_t)at.n);
     if (from >= to) return;

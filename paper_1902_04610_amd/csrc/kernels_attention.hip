@@ -11,14 +11,25 @@
 
 namespace salus {
 
-constexpr uint32_t kAttentionThreads = 256, kFewColumns = 16;
+constexpr uint32_t kAttentionThreads = 256, kFewColumns = 16, kManyFrom = 64;      // columns of a sequence, on average, from which on tiles are large
+constexpr uint32_t many_waves(uint32_t D) { return D <= 128 ? 8 : 4; }
+constexpr uint32_t many_columns(uint32_t D) { return 32 * many_waves(D); }
 constexpr int32_t kStride = 4 * (int32_t)kKeys;      // keys between two tiles of a wavefront
 
-AttentionParts attention_parts(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len)
+AttentionParts attention_parts(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len, uint32_t window)
 {
-    const uint64_t tiles = (uint64_t)ColumnBase<kFewColumns>{Hq / Hkv}(M, n_seqs) * Hkv, target = 1024;
-    const uint64_t part = std::max<uint64_t>(256, ((uint64_t)max_len * std::min(tiles, target) / target + 127) / 128 * 128);
-    return {(uint32_t)part, (uint32_t)((max_len + part - 1) / part)};
+    const uint32_t G = Hq / Hkv;
+    const bool many = (uint64_t)M * G >= (uint64_t)kManyFrom * n_seqs;
+    const uint32_t columns = many ? many_columns(D) : kFewColumns;
+    const uint64_t tiles = (uint64_t)ColumnBase{G, columns}(M, n_seqs) * Hkv, target = many ? 512 : 1024, least = many ? 512 : 256;
+    const auto part = [&](uint64_t keys) { return std::max<uint64_t>(least, (keys * std::min(tiles, target) / target + 127) / 128 * 128); };
+    const auto parts = [](uint64_t keys, uint64_t of) { return (keys + of - 1) / of; };
+    const uint64_t most = parts(max_len, part(max_len));      // what there is room for
+    // with a window a tile's keys are no more than this
+    const uint64_t keys = window ? std::min<uint64_t>(max_len, (uint64_t)window + columns / G + 32) : max_len;
+    uint64_t of = part(keys);
+    while (parts(keys, of) > most) of += 128;
+    return {columns, (uint32_t)of, (uint32_t)parts(keys, of)};
 }
 
 // of the parts of a row: D sums, the largest score and the sum of the weights
@@ -172,7 +183,7 @@ __global__ __launch_bounds__(kAttentionThreads, N <= 4 ? 2 : 1) void attend_few(
     AttentionProblem p;
     const uint32_t t = find_owner(a.first, a.p, a.base + blockIdx.x, p);
     ColumnTile tile;
-    if (!find_columns<kFewColumns>(p, t / p.parts, t % p.parts, tile) || tile.part >= max(tile.parts, 1u)) return;
+    if (!find_columns<false>(p, t / p.parts, t % p.parts, tile) || tile.part >= max(tile.parts, 1u)) return;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
     const uint32_t G = p.seq.Hq / p.seq.Hkv, column = min(tile.first + c, tile.end - 1), i = column / G;
     const bool valid = tile.first + c < tile.end;
@@ -265,17 +276,370 @@ __global__ __launch_bounds__(kAttentionThreads, N <= 4 ? 2 : 1) void attend_few(
     }
 }
 
-// The parts of every row that has several become one: a workgroup takes a tile of columns.
+// ---- many rows ----------------------------------------------------------------------------------------------------------------
+// Prompts and chunks of them: bound by the matrix pipes and by what the exponentials leave of them.  A workgroup's wavefronts have 32 columns each and share the tiles of keys and values, which
+// travel straight into LDS, as they lie in the cache, two stages ahead (v_mfma_f32_32x32x16_bf16; every read from LDS is 512 consecutive bytes for each half of
+// the lanes).  One barrier a stage: what it says is that all of the stage has landed and that the stage before it has been read.
+// The largest score is only followed when it grows by more than 2^8: sums stay far below the largest float, and are scaled hardly ever.
+constexpr float kGrowth = 8.0f;
+
+// Sixteen bytes a lane from base + from + off to LDS at `to` + 16 lane.  The scalars may come from lane reads: five wait states stand in front of their use.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ inline void dma16_page(uint32_t to, uint64_t base, uint32_t from, uint32_t off)
+{
+    const u32x4 buffer = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, kOutside, 0x00027000u};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(buffer), "s"(from) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+
+// Bits 2 and 3 exchanged: row m of a fragment is key (or element of a value) swap_rows(m) of its 32, so that a lane's eight sums in a row are of consecutive ones.
+__device__ inline uint32_t swap_rows(uint32_t m) { return (m & ~12u) | (m & 4u) << 1 | (m & 8u) >> 1; }
+
+__device__ inline float larger_half(float x)      // of lanes l and l + 32
+{
+    const uint32_t w = __builtin_bit_cast(uint32_t, x);
+    const auto both = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return fmaxf(as_float(both[0]), as_float(both[1]));
+}
+
+// Lane 32 h + c has of column c elements 32 i + 16 u + 8 h + e in o[i][8 u + e], and of a tile's scores those of keys 16 u + 8 h + e in x[8 u + e].
+template <int N>
+struct ManySums {
+    static constexpr uint32_t D = 32 * N;
+    f32x16 o[N];
+    float m = -INFINITY, l = 0.0f;
+
+    __device__ void follow(float top)
+    {
+        const float f = rescale(m, top);
+        m = top;
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[i][r] *= f;
+    }
+
+    // A lane's place in the fragments of keys and values.
+    __device__ static uint32_t key_at() { return (threadIdx.x & 32) * 16 + swap_rows(threadIdx.x & 31) * 16; }
+    __device__ static uint32_t value_at() { return (threadIdx.x & 32) / 32 * (D * 16) + swap_rows(threadIdx.x & 31) * 16; }
+
+    // The queries' fragments: what registers do not hold (rest) is kept in LDS, where each lane finds its own.
+    static constexpr int kHeld = N > 6 ? 12 : 2 * N, kRest = 2 * N - kHeld;
+
+    __device__ static f32x16 scores(const char *k, const u32x4 (&q)[kHeld], const char *rest)
+    {
+        f32x16 x = {};
+#pragma unroll
+        for (int i = 0; i < 2 * N; ++i) {
+            const u32x4 mine = i < kHeld ? q[i < kHeld ? i : 0] : *(const u32x4 *)(rest + (i - kHeld) * 1024);
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(k + i * 1024), as_fragment(mine), x, 0, 0, 0);
+            if constexpr (N > 6)
+                if (i % 4 == 3) asm volatile("" ::: "memory");      // not all of them at once: there are no registers for them
+        }
+        return x;
+    }
+
+    __device__ static void hide(f32x16 &x, Sight sight, int32_t key_0, bool there)
+    {
+        const int32_t key = key_0 + (int32_t)(threadIdx.x & 32) / 4;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (!there || !sight.sees(key + 16 * (r / 8) + r % 8)) x[r] = -INFINITY;
+    }
+
+    // The largest score so far, of the column.
+    __device__ float top_of(const f32x16 &x, float scale) const
+    {
+        float top = x[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, x[r]);
+        return fmaxf(m, larger_half(top) * scale);
+    }
+
+    __device__ void weigh(f32x16 &x, float scale)
+    {
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], scale, -base));
+            l += x[r];
+        }
+    }
+    __device__ static u32x4 packed(const f32x16 &x, int u)
+    {
+        return {bf16_pack(x[8 * u], x[8 * u + 1]), bf16_pack(x[8 * u + 2], x[8 * u + 3]), bf16_pack(x[8 * u + 4], x[8 * u + 5]), bf16_pack(x[8 * u + 6], x[8 * u + 7])};
+    }
+    __device__ static u32x4 value(const char *v, int i, int u) { return *(const u32x4 *)(v + (2 * u * D + 32 * i) * 16); }
+
+    // O^T += V^T P^T.
+    __device__ void add_values(const f32x16 &x, const char *v)
+    {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const u32x4 w = packed(x, u);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_fragment(value(v, i, u)), as_fragment(w), o[i], 0, 0, 0);
+                if constexpr (N > 6) asm volatile("" ::: "memory");
+            }
+        }
+    }
+
+    // The same for a tile of which not every column sees every key.  v: where the tile's values begin.  end: the first key that no column of the wavefront sees.
+    __device__ void add_seen_values(const f32x16 &x, const char *v, Sight sight, int32_t key_0, int32_t end)
+    {
+        const char *mine = v + value_at();
+        const int32_t left = end - key_0 - (int32_t)(threadIdx.x & 32) / 4;
+        const u32x4 meant[2] = {first_tokens(u32x4{~0u, ~0u, ~0u, ~0u}, left), first_tokens(u32x4{~0u, ~0u, ~0u, ~0u}, left - 16)};
+        uint32_t carried = 0;      // an exponent of ones carries into the bit above it
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll N > 6 ? 1 : N
+            for (int i = 0; i < N; ++i) {
+                const u32x4 w = value(mine, i, u);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) carried |= (w[e] & meant[u][e] & 0x7f807f80u) + 0x00800080u;
+            }
+        if (__any(carried & 0x80008000u)) {
+            add_one_by_one(x, v, sight, key_0);
+            return;
+        }
+        asm volatile("" ::: "memory");      // read again: there are no registers to keep them
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const u32x4 w = packed(x, u);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                u32x4 vs = value(mine, i, u);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vs[e] &= meant[u][e];
+                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_fragment(vs), as_fragment(w), o[i], 0, 0, 0);
+                if constexpr (N > 6) asm volatile("" ::: "memory");
+            }
+        }
+    }
+
+    // O^T += V^T P^T key by key, leaving out what a column does not see.
+    __device__ void add_one_by_one(const f32x16 &x, const char *v, Sight sight, int32_t key_0)
+    {
+        const uint32_t lane = threadIdx.x & 63, h = lane >> 5;
+#pragma unroll 1
+        for (uint32_t key = 0; key < kKeys; ++key) {
+            float w = x[0];
+#pragma unroll
+            for (uint32_t r = 1; r < 16; ++r) w = key / 16 * 8 + key % 8 == r ? x[r] : w;
+            w = __shfl(w, (lane & 31) + key / 8 % 2 * 32, 64);
+            const bool seen = sight.sees(key_0 + (int32_t)key);
+            if (!__any(seen)) continue;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float value = bf16_low(*(const uint16_t *)(v + (((key / 8) * D + 32 * i + 16 * (r / 8) + 8 * h + r % 8) * 8 + key % 8) * 2));
+                    if (seen) o[i][r] = fmaf(w, value, o[i][r]);
+                    if (r % 2 == 1) asm volatile("" ::: "memory");      // a few loads at a time: registers for all would be taken from the loop that matters
+                }
+        }
+    }
+};
+
+template <int N, typename Args>
+__global__ __launch_bounds__(64 * many_waves(32 * N), N == 1 ? 4 : many_waves(32 * N) / 4) void attend_many(Args a)
+{
+    // Tiles of a stage, stages that are asked for ahead; a stage is entered while the values of the tile in front of it are still to be read.
+    constexpr uint32_t D = 32 * N, WAVES = many_waves(D), TILES = N <= 4 ? 4 : N == 6 ? 2 : 1, AHEAD = N <= 6 ? 1 : 2, RING = TILES * (1 + AHEAD) + 1;
+    constexpr uint32_t kTile = 64 * D, kAsks = TILES * 2 * kTile / 1024 / WAVES;      // bytes of a tile's keys, or values; a wavefront's requests of 1 KB a stage
+    __shared__ __attribute__((aligned(1024))) char smem[RING * 2 * kTile + WAVES * ManySums<N>::kRest * 1024];
+    AttentionProblem p;
+    const uint32_t t = find_owner(a.first, a.p, a.base + blockIdx.x, p);
+    ColumnTile tile;
+    if (!find_columns<true>(p, t / p.parts, t % p.parts, tile) || tile.part >= max(tile.parts, 1u)) return;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, c = lane & 31;
+    const uint32_t G = p.seq.Hq / p.seq.Hkv, first = tile.first + 32 * wave, column = min(first + c, tile.end - 1), i = column / G;
+    const bool valid = first + c < tile.end;
+    const uint64_t row = (uint64_t)(tile.row + i) * p.seq.Hq + tile.head * G + column % G;
+    using Sums = ManySums<N>;
+    u32x4 q[Sums::kHeld];
+    char *rest = smem + RING * 2 * kTile + wave * Sums::kRest * 1024 + lane * 16;
+#pragma unroll
+    for (int k = 0; k < 2 * N; ++k) {
+        const u32x4 w = *(const Global<u32x4> *)((const Global<char> *)p.q + row * (D * 2) + 32 * k + 16 * h);
+        if (k < Sums::kHeld) q[k < Sums::kHeld ? k : 0] = w;
+        else *(u32x4 *)(rest + (k - Sums::kHeld) * 1024) = w;
+    }
+    const Sight sight = sight_of(p, tile.position + (int32_t)i);
+    // what all columns of the wavefront see, and the keys between which any sees one
+    const uint32_t last_row = (min(first + 32, tile.end) - 1) / G;
+    const Sight every = {sight_of(p, tile.position + (int32_t)last_row).low, tile.position + (int32_t)(min(first, tile.end - 1) / G)};
+    const int32_t none = first < tile.end ? tile.position + (int32_t)last_row + 1 : 0, low = sight_of(p, every.high).low;
+
+    ManySums<N> s;
+#pragma unroll
+    for (int k = 0; k < N; ++k) s.o[k] = f32x16{};
+    const int32_t from = tile.key + (int32_t)(tile.part * p.part), end = min(tile.key_end, from + (int32_t)p.part);
+    const uint32_t tiles = end > from ? (uint32_t)(end - from + 31) / 32 : 0, stages = (tiles + TILES - 1) / TILES;
+    const Global<int32_t> *table = (const Global<int32_t> *)p.seq.table + (uint64_t)tile.s * p.seq.max_pages;
+    const uint32_t lds = lds_address(smem);
+    // a stage is 2 TILES halves (a tile's keys, its values), each a share of the wavefronts'
+    constexpr uint32_t kSharers = WAVES / (2 * TILES);
+    const uint32_t half = wave / kSharers, share = wave % kSharers * kAsks;
+    const uint64_t k_cache = (uint64_t)(uintptr_t)p.k, v_cache = (uint64_t)(uintptr_t)p.v, cache = half & 1 ? v_cache : k_cache;
+    // lane l: page of tile (known + l), the ones that are asked for and the ones that are worked on
+    int32_t pages = 0, pages_before = 0;
+    uint32_t known = ~0u;
+    bool missing = false;        // a page that is not there has been met
+    const auto page_of = [&](uint32_t number) __attribute__((always_inline)) {
+        return number >= known ? __builtin_amdgcn_readlane(pages, (number - known) & 63) : __builtin_amdgcn_readlane(pages_before, (number + 64 - known) & 63);
+    };
+    const auto there = [&](int32_t page) { return page >= 0 && (uint32_t)page < p.seq.n_pages; };
+    // A stage's requests are made a few at a time: all at once they would keep every wavefront waiting until the addresses of most have been worked through.
+    uint64_t ask_base = 0;
+    uint32_t ask_to = 0, asked = kAsks;
+    const auto aim = [&](uint32_t stage) __attribute__((always_inline)) {
+        if (stage * TILES % 64 == 0) {
+            pages_before = pages;
+            known = stage * TILES;
+            const uint32_t of = (uint32_t)(from + 32 * (int32_t)min(known + lane, tiles - 1)) >> p.seq.page_bits;
+            pages = of < p.seq.max_pages ? table[of] : -1;
+            missing = missing || __any(!there(pages));
+            asm volatile("" : "+v"(pages));      // waited for here, where it is asked for: else the compiler waits, for all requests there are, wherever a page is looked up
+        }
+        const uint32_t place = stage * TILES + half / 2, number = min(place, tiles - 1), key = (uint32_t)from + 32 * number;
+        int32_t page = page_of(number);
+        if (!there(page)) page = 0;      // something to load: nobody looks at it
+        ask_base = uniform64(cache + (((uint64_t)(uint32_t)page * p.seq.Hkv + tile.head) << p.seq.page_bits) * (2 * D) +
+                             (uint64_t)((key & ((1u << p.seq.page_bits) - 1)) / 32) * kTile);
+        ask_to = __builtin_amdgcn_readfirstlane(lds + (place % RING * 2 + (half & 1)) * kTile);
+        asked = 0;
+    };
+    const auto ask = [&](uint32_t up_to) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (; asked < min(up_to, kAsks); ++asked) dma16_page(ask_to + (share + asked) * 1024, ask_base, (share + asked) * 1024, lane * 16);
+    };
+    // A stage is there, and all wavefronts are through with what the next one that is asked for takes the place of.
+    const auto enter = [&](uint32_t stage) __attribute__((always_inline)) {
+        stage = __builtin_amdgcn_readfirstlane(stage);
+        ask(kAsks);
+        if (AHEAD > 1 && stage + 1 < stages) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * kAsks) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (stage + AHEAD < stages) aim(stage + AHEAD);
+    };
+    for (uint32_t stage = 0; stage < min(AHEAD, stages); ++stage) {
+        aim(stage);
+        ask(kAsks);
+    }
+    // this wavefront's tiles
+    const int32_t seen_end = min(end, none);
+    uint32_t n = low + 1 > from ? (uint32_t)(low + 1 - from) / 32 : 0;
+    const uint32_t n_end = seen_end > from ? (uint32_t)(seen_end - from + 31) / 32 : 0;
+    uint32_t entered = 0;
+    const auto keys = [&](uint32_t number) { return smem + number % RING * (2 * kTile); };
+    const auto key_of = [&](uint32_t number) { return from + 32 * (int32_t)number; };
+    // tiles in front of this one are seen whole by all columns as far as the window goes
+    const uint32_t whole_end = every.high + 1 > from ? min((uint32_t)(every.high + 1 - from) / 32, n_end) : 0;
+    const auto whole = [&](uint32_t number) { return key_of(number) > every.low && key_of(number) + 31 <= every.high && there(page_of(number)); };
+    if (n < n_end) {
+        const uint32_t key_at = s.key_at(), value_at = s.value_at();
+        for (; entered <= n / TILES; ++entered) enter(entered);
+        f32x16 x = s.scores(keys(n) + key_at, q, rest);
+        bool all = whole(n);
+        if (!all) s.hide(x, sight, key_of(n), there(page_of(n)));
+        float top = s.top_of(x, p.scale);
+        if (__any(top > s.m)) s.follow(top);
+        for (;;) {
+            // Tiles that all columns see whole: the next tile's scores are multiplied while this one's weights are made, whose reads from LDS are asked for in front of both.
+            bool grown = false;
+            if constexpr (N <= 4) {
+#pragma unroll 1
+                while (all && n + 1 < whole_end && !missing) {
+                    if ((n + 1) % TILES == 0) enter(entered++);
+                    const char *k = keys(n + 1) + key_at, *v = keys(n) + kTile + value_at;
+                    u32x4 ks[2 * N], vs[2][N], w[2];
+#pragma unroll
+                    for (int j = 0; j < 2 * N; ++j) ks[j] = *(const u32x4 *)(k + j * 1024);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int j = 0; j < N; ++j) vs[u][j] = s.value(v, j, u);
+                    ask(asked + (kAsks + 2) / 3);
+                    __builtin_amdgcn_sched_barrier(0);
+                    s.weigh(x, p.scale);
+                    w[0] = s.packed(x, 0);
+                    w[1] = s.packed(x, 1);
+                    f32x16 y = {};
+#pragma unroll
+                    for (int j = 0; j < 2 * N; ++j) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_fragment(ks[j]), as_fragment(q[j]), y, 0, 0, 0);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int j = 0; j < N; ++j) s.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_fragment(vs[u][j]), as_fragment(w[u]), s.o[j], 0, 0, 0);
+                    x = y;
+                    ++n;
+                    top = s.top_of(x, p.scale);
+                    grown = __any(top > s.m + kGrowth);
+                    if (grown) break;
+                }
+            }
+            if (grown) {
+                s.follow(top);
+                continue;
+            }
+            // the others, and the last one
+            const bool more = n + 1 < n_end;
+            if (more && (n + 1) % TILES == 0) enter(entered++);
+            s.weigh(x, p.scale);
+            if (all) s.add_values(x, keys(n) + kTile + value_at);
+            else s.add_seen_values(x, keys(n) + kTile, sight, key_of(n), there(page_of(n)) ? none : 0);
+            if (!more) break;
+            ++n;
+            x = s.scores(keys(n) + key_at, q, rest);
+            all = whole(n);
+            if (!all) s.hide(x, sight, key_of(n), there(page_of(n)));
+            top = s.top_of(x, p.scale);
+            if (__any(top > s.m + kGrowth)) s.follow(top);
+        }
+    }
+    for (; entered < stages; ++entered) enter(entered);
+    if (!valid) return;
+    s.l += __shfl_xor(s.l, 32, 64);
+    if (tile.parts > 1) {
+        Global<float> *to = (Global<float> *)p.work + (row * p.parts + tile.part) * (D + 2);
+        if (h == 0) {
+            to[D] = s.m;
+            to[D + 1] = s.l;
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) to[32 * k + 16 * (r / 8) + 8 * h + r % 8] = s.o[k][r];
+        return;
+    }
+    const float f = s.l == 0.0f ? 0.0f : 1.0f / s.l;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            u32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = bf16_pack(s.o[k][8 * u + 2 * e] * f, s.o[k][8 * u + 2 * e + 1] * f);
+            *(Global<u32x4> *)((Global<char> *)p.y + row * (D * 2) + (32 * k + 16 * u + 8 * h) * 2) = w;
+        }
+}
+
+// The parts of every row that has several become one: a workgroup takes sixteen columns.
 template <typename Args>
 __global__ __launch_bounds__(kAttentionThreads) void join_parts(Args a)
 {
     AttentionProblem p;
     const uint32_t t = find_owner(a.first, a.p, a.base + blockIdx.x, p);
     ColumnTile tile;
-    if (!find_columns<kFewColumns>(p, t, 0, tile) || tile.parts < 2) return;
-    const uint32_t D = p.seq.D, units = D / 2, G = p.seq.Hq / p.seq.Hkv;
-    for (uint32_t at = threadIdx.x; at < (tile.end - tile.first) * units; at += kAttentionThreads) {
-        const uint32_t column = tile.first + at / units, d = at % units * 2;
+    const uint32_t pieces = p.columns / kFewColumns;
+    if (!find_columns<false>(p, t / pieces, 0, tile) || tile.parts < 2) return;
+    const uint32_t D = p.seq.D, units = D / 2, G = p.seq.Hq / p.seq.Hkv, first = tile.first + t % pieces * kFewColumns, end = min(first + kFewColumns, tile.end);
+    for (uint32_t at = threadIdx.x; first + at / units < end; at += kAttentionThreads) {
+        const uint32_t column = first + at / units, d = at % units * 2;
         const uint64_t row = (uint64_t)(tile.row + column / G) * p.seq.Hq + tile.head * G + column % G;
         const Global<float> *from = (const Global<float> *)p.work + row * p.parts * (D + 2);
         float m = -INFINITY, l = 0.0f, low = 0.0f, high = 0.0f;
@@ -294,43 +658,52 @@ __global__ __launch_bounds__(kAttentionThreads) void join_parts(Args a)
 namespace {
 
 template <int N, uint32_t NP>
-hipError_t launch_few(const AttentionProblem *p, uint32_t n, hipStream_t stream, uint64_t *launches)
+hipError_t launch_width(const AttentionProblem *p, uint32_t n, bool many, hipStream_t stream, uint64_t *launches)
 {
-    return launch_answer_of<AttentionProblem, NP>(attend_few<N>, kAttentionThreads, p, n, stream, launches,
-                                                  [](const AttentionProblem &q) { return column_tiles<kFewColumns>(q) * q.parts; });
+    const auto tiles = [](const AttentionProblem &q) { return column_tiles(q) * q.parts; };
+    if (many) return launch_answer_of<AttentionProblem, NP>(attend_many<N>, 64 * many_waves(32 * N), p, n, stream, launches, tiles);
+    return launch_answer_of<AttentionProblem, NP>(attend_few<N>, kAttentionThreads, p, n, stream, launches, tiles);
 }
 
 template <uint32_t NP>
-hipError_t launch_all(const std::vector<AttentionProblem> *by_width, hipStream_t stream, uint64_t *launches)
+hipError_t launch_parts(const AttentionProblem *p, uint32_t n, uint32_t width, bool many, hipStream_t stream, uint64_t *launches)
 {
-    hipError_t e = hipSuccess;
-    const auto run = [&](int width, hipError_t (*launch)(const AttentionProblem *, uint32_t, hipStream_t, uint64_t *)) {
-        if (e == hipSuccess && !by_width[width].empty()) e = launch(by_width[width].data(), (uint32_t)by_width[width].size(), stream, launches);
-    };
-    run(1, launch_few<1, NP>);
-    run(2, launch_few<2, NP>);
-    run(3, launch_few<3, NP>);
-    run(4, launch_few<4, NP>);
-    run(6, launch_few<6, NP>);
-    run(8, launch_few<8, NP>);
-    return e;
+    switch (width) {
+    case 32: return launch_width<1, NP>(p, n, many, stream, launches);
+    case 64: return launch_width<2, NP>(p, n, many, stream, launches);
+    case 96: return launch_width<3, NP>(p, n, many, stream, launches);
+    case 128: return launch_width<4, NP>(p, n, many, stream, launches);
+    case 192: return launch_width<6, NP>(p, n, many, stream, launches);
+    default: return launch_width<8, NP>(p, n, many, stream, launches);
+    }
 }
 
 }  // namespace
 
 hipError_t launch_attention(const AttentionProblem *p, uint32_t n, hipStream_t stream, uint64_t *launches)
 {
-    std::vector<AttentionProblem> by_width[9], parted;
-    for (uint32_t i = 0; i < n; ++i) {
-        by_width[p[i].seq.D / 32].push_back(p[i]);
-        if (p[i].parts > 1) parted.push_back(p[i]);
-    }
-    const hipError_t e = n <= kAnswerFew ? launch_all<kAnswerFew>(by_width, stream, launches) : launch_all<kAnswerProblems>(by_width, stream, launches);
-    if (e != hipSuccess || parted.empty()) return e;
-    const uint32_t count = (uint32_t)parted.size();
-    if (count <= kAnswerFew)
-        return launch_answer_of<AttentionProblem, kAnswerFew>(join_parts, kAttentionThreads, parted.data(), count, stream, launches, column_tiles<kFewColumns>);
-    return launch_answer_of<AttentionProblem, kAnswerProblems>(join_parts, kAttentionThreads, parted.data(), count, stream, launches, column_tiles<kFewColumns>);
+    // a launch for each width and kind that is there
+    std::vector<AttentionProblem> group;
+    group.reserve(n);
+    for (uint32_t width = 32; width <= 256; width += 32)
+        for (int many = 0; many < 2; ++many) {
+            group.clear();
+            for (uint32_t i = 0; i < n; ++i)
+                if (p[i].seq.D == width && (p[i].columns != kFewColumns) == (many != 0)) group.push_back(p[i]);
+            if (group.empty()) continue;
+            const uint32_t count = (uint32_t)group.size();
+            const hipError_t e = count <= kAnswerFew ? launch_parts<kAnswerFew>(group.data(), count, width, many, stream, launches)
+                                                     : launch_parts<kAnswerProblems>(group.data(), count, width, many, stream, launches);
+            if (e != hipSuccess) return e;
+        }
+    group.clear();
+    for (uint32_t i = 0; i < n; ++i)
+        if (p[i].parts > 1) group.push_back(p[i]);
+    const uint32_t count = (uint32_t)group.size();
+    if (count == 0) return hipSuccess;
+    const auto pieces = [](const AttentionProblem &q) { return column_tiles(q) * (q.columns / kFewColumns); };
+    if (count <= kAnswerFew) return launch_answer_of<AttentionProblem, kAnswerFew>(join_parts, kAttentionThreads, group.data(), count, stream, launches, pieces);
+    return launch_answer_of<AttentionProblem, kAnswerProblems>(join_parts, kAttentionThreads, group.data(), count, stream, launches, pieces);
 }
 
 }  // namespace salus

@@ -411,27 +411,25 @@ __device__ inline int32_t choose_in(const LogitRow &row, const RowLimits &l, uin
     }
     if (threadIdx.x == 0) c.token = (int32_t)first;
     __syncthreads();
-    if (wave != 0) {
-        __syncthreads();
-        return c.token;
-    }
     // runs of sums: one wavefront finds whose token it is, and the token
     n *= kSampleWaves;
     constexpr uint32_t kEach = kPieceSums * kSampleWaves / 64;
-    uint64_t mine = 0;
-    for (uint32_t i = 0; i < kEach; ++i) mine += kEach * lane + i < n ? c.sums[kEach * lane + i] : 0;
-    const uint64_t scan = wave_sum_scan(mine), all = lane_value(scan, 63);
-    if (all != 0) {
-        // (the sums of pieces are rounded otherwise: the last token that weighs anything if none passes)
-        const uint64_t want = min((uint64_t)(fmax(left, 0.0) * kWeightUnit), all - 1);
-        const uint32_t owner = __builtin_ctzll(__ballot(scan > want));
-        uint64_t before = lane_value(scan - mine, owner);
-        uint32_t run = kEach * owner;
-        while (before + c.sums[run] <= want) before += c.sums[run++];
-        const uint32_t i = from + run * 64 + lane;
-        const uint64_t w = i < to ? l.kept(row[i], i) : 0;
-        const uint64_t past = __ballot(before + wave_sum_scan(w) > want);
-        if (lane == 0) c.token = (int32_t)(from + run * 64 + __builtin_ctzll(past));
+    if (wave == 0) {
+        uint64_t mine = 0;
+        for (uint32_t i = 0; i < kEach; ++i) mine += kEach * lane + i < n ? c.sums[kEach * lane + i] : 0;
+        const uint64_t scan = wave_sum_scan(mine), all = lane_value(scan, 63);
+        if (all != 0) {
+            // (the sums of pieces are rounded otherwise: the last token that weighs anything if none passes)
+            const uint64_t want = min((uint64_t)(fmax(left, 0.0) * kWeightUnit), all - 1);
+            const uint32_t owner = __builtin_ctzll(__ballot(scan > want));
+            uint64_t before = lane_value(scan - mine, owner);
+            uint32_t run = kEach * owner;
+            while (before + c.sums[run] <= want) before += c.sums[run++];
+            const uint32_t i = from + run * 64 + lane;
+            const uint64_t w = i < to ? l.kept(row[i], i) : 0;
+            const uint64_t past = __ballot(before + wave_sum_scan(w) > want);
+            if (lane == 0) c.token = (int32_t)(from + run * 64 + __builtin_ctzll(past));
+        }
     }
     __syncthreads();
     return c.token;
