@@ -16,13 +16,20 @@ constexpr uint32_t many_waves(uint32_t D) { return D <= 128 ? 8 : 4; }
 constexpr uint32_t many_columns(uint32_t D) { return 32 * many_waves(D); }
 constexpr int32_t kStride = 4 * (int32_t)kKeys;      // keys between two tiles of a wavefront
 
+// Few rows, one sequence of 8 key heads of 128, us for 500 / 1000 / 4000 / 16000 keys: parts of 256 10.6 11.1 11.4 19.9, of 512 8.4 12.3 12.6 18.9, of 1024 8.4
+// 10.8 16.5 19.5: up to kWhole keys a second launch costs more than it saves.  16 such sequences, 1000 / 2000 keys: 18.5 28.9, 20.7 28.5, 16.2 32.6; 16 jobs,
+// 136 sequences of 1 .. 6000 keys: 80, 67, 63.  The rule knows the job alone, not the call's others: what a job is answered does not depend on its neighbours.
+constexpr uint32_t kWhole = 1024, kLeastPart = 512, kTarget = 512;
+
 AttentionParts attention_parts(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len, uint32_t window)
 {
     const uint32_t G = Hq / Hkv;
     const bool many = (uint64_t)M * G >= (uint64_t)kManyFrom * n_seqs;
     const uint32_t columns = many ? many_columns(D) : kFewColumns;
-    const uint64_t tiles = (uint64_t)ColumnBase{G, columns}(M, n_seqs) * Hkv, target = many ? 512 : 1024, least = many ? 512 : 256;
-    const auto part = [&](uint64_t keys) { return std::max<uint64_t>(least, (keys * std::min(tiles, target) / target + 127) / 128 * 128); };
+    const uint64_t tiles = (uint64_t)ColumnBase{G, columns}(M, n_seqs) * Hkv;
+    const auto part = [&](uint64_t keys) {
+        return keys <= kWhole ? kWhole : std::max<uint64_t>(kLeastPart, (keys * std::min<uint64_t>(tiles, kTarget) / kTarget + 127) / 128 * 128);
+    };
     const auto parts = [](uint64_t keys, uint64_t of) { return (keys + of - 1) / of; };
     const uint64_t most = parts(max_len, part(max_len));      // what there is room for
     // with a window a tile's keys are no more than this
@@ -74,8 +81,9 @@ struct FewLoads {
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int u = 0; u < 2; ++u) t.k[i][u] = *(const Global<u32x4> *)(k + k_at + i * 2048 + u * 64);
+        // read once: past the caches (306 us against 337 for 1.9 GB); keys, whose lines two loads share, through them
 #pragma unroll
-        for (int i = 0; i < 2 * N; ++i) t.v[i] = *(const Global<u32x4> *)(v + v_at + i * 256);
+        for (int i = 0; i < 2 * N; ++i) t.v[i] = __builtin_nontemporal_load((const Global<u32x4> *)(v + v_at + i * 256));
     }
 };
 
@@ -628,30 +636,97 @@ __global__ __launch_bounds__(64 * many_waves(32 * N), N == 1 ? 4 : many_waves(32
         }
 }
 
-// The parts of every row that has several become one: a workgroup takes sixteen columns.
+// The parts of every row that has several become one.  From 17 parts on a workgroup takes a column, its wavefronts a quarter of the parts each, its lanes the
+// elements; below that it takes 16 columns, a thread four elements of one.
+// 64 columns of 64 parts 6.6 us (16 with a wavefront to a column); 1088 columns of up to 12 parts 5.4 us; 32768 columns of 2 - 3 parts of 64 11.3 us.
+constexpr uint32_t kFewParts = 16;
+__host__ __device__ inline uint32_t join_columns(uint32_t parts) { return parts > kFewParts ? 1 : 16; }
+
+__device__ inline void join_column(const AttentionProblem &p, uint64_t row, uint32_t parts, float (&sums)[4][256])
+{
+    constexpr uint32_t kAtOnce = 8;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), D = p.seq.D;
+    const Global<float> *from = (const Global<float> *)p.work + row * p.parts * (D + 2);
+    // each wavefront has the largest score of all parts, and the weights of its own: lane i of part begin + i
+    float m = -INFINITY, l = 0.0f, sum[4] = {};
+    for (uint32_t i = lane; i < parts; i += 64) m = fmaxf(m, from[(uint64_t)i * (D + 2) + D]);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    for (uint32_t i = lane; i < parts; i += 64) l = fmaf(from[(uint64_t)i * (D + 2) + D + 1], rescale(from[(uint64_t)i * (D + 2) + D], m), l);
+    l = wave_total(l);
+    const uint32_t begin = parts * wave / 4, end = parts * (wave + 1) / 4;
+    for (uint32_t first = begin; first < end; first += 64) {
+        const uint32_t n = min(end - first, 64u);
+        const float top = from[(uint64_t)(first + min(lane, n - 1)) * (D + 2) + D], f = lane < n ? rescale(top, m) : 0.0f;
+        for (uint32_t i = 0; i < n; i += kAtOnce) {
+            float o[kAtOnce][4];
+#pragma unroll
+            for (uint32_t j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) o[j][k] = i + j < n && lane + 64 * k < D ? from[(uint64_t)(first + i + j) * (D + 2) + lane + 64 * k] : 0.0f;
+#pragma unroll
+            for (uint32_t j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) sum[k] = fmaf(o[j][k], i + j < n ? lane_value(f, (i + j) & 63) : 0.0f, sum[k]);
+        }
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) sums[wave][lane + 64 * k] = sum[k];
+    __syncthreads();
+    const uint32_t e = threadIdx.x;
+    if (e < D) {
+        const float all = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+        ((Global<uint16_t> *)p.y)[row * D + e] = (uint16_t)bf16_bits(l == 0.0f ? 0.0f : all * (1.0f / l));
+    }
+}
+
 template <typename Args>
 __global__ __launch_bounds__(kAttentionThreads) void join_parts(Args a)
 {
+    __shared__ union {
+        float share[16][kFewParts];             // of a part in its column
+        float sums[4][256];
+    } lds;
     AttentionProblem p;
-    const uint32_t t = find_owner(a.first, a.p, a.base + blockIdx.x, p);
+    const uint32_t t = find_owner(a.first, a.p, a.base + blockIdx.x, p), each = join_columns(p.parts), pieces = p.columns / each;
     ColumnTile tile;
-    const uint32_t pieces = p.columns / kFewColumns;
     if (!find_columns<false>(p, t / pieces, 0, tile) || tile.parts < 2) return;
-    const uint32_t D = p.seq.D, units = D / 2, G = p.seq.Hq / p.seq.Hkv, first = tile.first + t % pieces * kFewColumns, end = min(first + kFewColumns, tile.end);
-    for (uint32_t at = threadIdx.x; first + at / units < end; at += kAttentionThreads) {
-        const uint32_t column = first + at / units, d = at % units * 2;
-        const uint64_t row = (uint64_t)(tile.row + column / G) * p.seq.Hq + tile.head * G + column % G;
-        const Global<float> *from = (const Global<float> *)p.work + row * p.parts * (D + 2);
-        float m = -INFINITY, l = 0.0f, low = 0.0f, high = 0.0f;
-        for (uint32_t i = 0; i < tile.parts; ++i) m = fmaxf(m, from[i * (D + 2) + D]);
-        for (uint32_t i = 0; i < tile.parts; ++i) {
-            const float f = rescale(from[i * (D + 2) + D], m);
-            l = fmaf(from[i * (D + 2) + D + 1], f, l);
-            low = fmaf(from[i * (D + 2) + d], f, low);
-            high = fmaf(from[i * (D + 2) + d + 1], f, high);
+    const uint32_t G = p.seq.Hq / p.seq.Hkv, D = p.seq.D, first = tile.first + t % pieces * each;
+    if (first >= tile.end) return;
+    const auto row_of = [&](uint32_t column) { return (uint64_t)(tile.row + column / G) * p.seq.Hq + tile.head * G + column % G; };
+    if (each == 1) {
+        join_column(p, row_of(first), tile.parts, lds.sums);
+        return;
+    }
+    const uint32_t n = min(tile.end - first, 16u), stride = p.parts * (D + 2), i = threadIdx.x % 16;
+    {
+        const uint32_t c = threadIdx.x / 16;
+        const Global<float> *of = (const Global<float> *)p.work + row_of(first + min(c, n - 1)) * stride + min(i, tile.parts - 1) * (D + 2) + D;
+        const float top = of[0], weight = of[1];
+        float m = top;
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+        const float f = i < tile.parts ? rescale(top, m) : 0.0f;
+        float l = weight * f;
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+        lds.share[c][i] = l == 0.0f ? 0.0f : f / l;
+    }
+    __syncthreads();
+    for (uint32_t at = threadIdx.x; at < n * (D / 4); at += kAttentionThreads) {
+        const uint32_t c = at / (D / 4), e = at % (D / 4) * 4;
+        const uint64_t row = row_of(first + c);
+        const Global<float> *of = (const Global<float> *)p.work + row * stride + e;
+        float sum[4] = {};
+        for (uint32_t j = 0; j < tile.parts; j += 2) {
+            const bool more = j + 1 < tile.parts;
+            const Global<u32x2> *one = (const Global<u32x2> *)(of + j * (D + 2)), *two = (const Global<u32x2> *)(of + (j + more) * (D + 2));
+            const u32x2 v[4] = {one[0], one[1], two[0], two[1]};
+            const float f = lds.share[c][j], h = more ? lds.share[c][j + 1] : 0.0f;
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) sum[k] = fmaf(as_float(v[2 + k / 2][k % 2]), h, fmaf(as_float(v[k / 2][k % 2]), f, sum[k]));
         }
-        const float f = l == 0.0f ? 0.0f : 1.0f / l;
-        *(Global<uint32_t> *)((Global<char> *)p.y + row * (D * 2) + d * 2) = bf16_pack(low * f, high * f);
+        *(Global<u32x2> *)((Global<char> *)p.y + row * (D * 2) + e * 2) = u32x2{bf16_pack(sum[0], sum[1]), bf16_pack(sum[2], sum[3])};
     }
 }
 
@@ -701,7 +776,7 @@ hipError_t launch_attention(const AttentionProblem *p, uint32_t n, hipStream_t s
         if (p[i].parts > 1) group.push_back(p[i]);
     const uint32_t count = (uint32_t)group.size();
     if (count == 0) return hipSuccess;
-    const auto pieces = [](const AttentionProblem &q) { return column_tiles(q) * (q.columns / kFewColumns); };
+    const auto pieces = [](const AttentionProblem &q) { return column_tiles(q) * (q.columns / join_columns(q.parts)); };
     if (count <= kAnswerFew) return launch_answer_of<AttentionProblem, kAnswerFew>(join_parts, kAttentionThreads, group.data(), count, stream, launches, pieces);
     return launch_answer_of<AttentionProblem, kAnswerProblems>(join_parts, kAttentionThreads, group.data(), count, stream, launches, pieces);
 }
