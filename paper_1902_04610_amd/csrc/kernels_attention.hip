@@ -721,7 +721,8 @@ __global__ __launch_bounds__(kAttentionThreads) void join_parts(Args a)
         for (uint32_t j = 0; j < tile.parts; j += 2) {
             const bool more = j + 1 < tile.parts;
             const Global<u32x2> *one = (const Global<u32x2> *)(of + j * (D + 2)), *two = (const Global<u32x2> *)(of + (j + more) * (D + 2));
-            const u32x2 v[4] = {one[0], one[1], two[0], two[1]};
+            // zero times what is no number would be none
+            const u32x2 none = {0u, 0u}, v[4] = {one[0], one[1], more ? two[0] : none, more ? two[1] : none};
             const float f = lds.share[c][j], h = more ? lds.share[c][j + 1] : 0.0f;
 #pragma unroll
             for (uint32_t k = 0; k < 4; ++k) sum[k] = fmaf(as_float(v[2 + k / 2][k % 2]), h, fmaf(as_float(v[k / 2][k % 2]), f, sum[k]));
