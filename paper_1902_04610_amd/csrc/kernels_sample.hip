@@ -404,10 +404,20 @@ __device__ inline int32_t choose_in(const LogitRow &row, const RowLimits &l, uin
     __syncthreads();
     uint32_t n = 0;
 #pragma unroll 1
-    for (uint32_t at = from; at < to; at += kSampleThreads, ++n) {
-        const uint32_t i = at + threadIdx.x;
-        const uint64_t sum = wave_total(i < to ? l.kept(row[i], i) : 0);
-        if (lane == 0) c.sums[n * kSampleWaves + wave] = sum;
+    for (uint32_t at = from; at < to; at += 8 * kSampleThreads) {
+        float x[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) {
+            const uint32_t i = at + k * kSampleThreads + threadIdx.x;
+            x[k] = i < to ? row[i] : -INFINITY;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) {
+            if (at + k * kSampleThreads >= to) break;
+            const uint64_t sum = wave_total(l.kept(x[k], at + k * kSampleThreads + threadIdx.x));
+            if (lane == 0) c.sums[n * kSampleWaves + wave] = sum;
+            ++n;
+        }
     }
     if (threadIdx.x == 0) c.token = (int32_t)first;
     __syncthreads();
@@ -441,8 +451,13 @@ __device__ inline int32_t choose_by_runs(const LogitRow &row, const RowParams &q
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, run = (row.V + kSampleThreads - 1) / kSampleThreads * 64;
     const uint32_t from = min(wave * run, row.V), to = min(from + run, row.V);
     uint64_t sum = 0;
+#pragma unroll 1
+    for (uint32_t unit = from / 8 + lane; unit < (to + 7) / 8; unit += 64) {
+        float x[8];
+        row.convert(row.raw(unit), unit, x);
 #pragma unroll 2
-    for (uint32_t i = from + lane; i < to; i += 64) sum += l.kept(row[i], i);
+        for (uint32_t i = 0; i < 8; ++i) sum += l.kept(x[i], unit * 8 + i);
+    }
     sum = wave_total(sum);
     __syncthreads();
     if (lane == 0) c.part[wave] = sum;
@@ -462,11 +477,11 @@ __device__ inline uint64_t block_total(uint64_t v, ChooseShared &c)
     return all;
 }
 
-// The place of the token with which the first ones of the row's order reach `target`, tokens or weight, among those down to l.cut.
-__device__ inline uint64_t reach(const LogitRow &row, const RowLimits &l, bool by_weight, uint64_t target, ChooseShared &c)
+// The place of the token with which the first ones of an order reach `target`, tokens or weight, among those whose places begin with `prefix` in front of the last
+// `left` bits.  each(f) calls f for each of a thread's tokens.
+template <typename Each>
+__device__ inline uint64_t reach(const Each &each, const RowLimits &l, bool by_weight, uint64_t target, uint64_t prefix, uint32_t left, ChooseShared &c)
 {
-    uint64_t prefix = 0;                     // the bits known so far
-    uint32_t left = kPlaceBits;
     for (;;) {
         const uint32_t bits = min(left, 11u), rest = left - bits;
         for (uint32_t i = threadIdx.x; i < kBins; i += kSampleThreads) {
@@ -474,15 +489,12 @@ __device__ inline uint64_t reach(const LogitRow &row, const RowLimits &l, bool b
             c.count[i] = 0;
         }
         __syncthreads();
-#pragma unroll 1
-        for (uint32_t i = threadIdx.x; i < row.V; i += kSampleThreads) {
-            const float x = row[i];
-            const uint64_t place = place_of(x, i);
-            if (x == -INFINITY || place < l.cut || (left < kPlaceBits && place >> left != prefix)) continue;
+        each([&](uint64_t place) {
+            if (left < kPlaceBits && place >> left != prefix) return;
             const uint32_t bin = kBins - 1 - ((uint32_t)(place >> rest) & ((1u << bits) - 1));
             atomicAdd(&c.count[bin], 1u);
-            if (by_weight) atomicAdd(&c.mass[bin], (unsigned long long)l.units(l.weight(x)));
-        }
+            if (by_weight) atomicAdd(&c.mass[bin], (unsigned long long)l.units(l.weight(logit_of(place))));
+        });
         __syncthreads();
         // two bins a thread, the earliest tokens in front
         const uint32_t b = 2 * threadIdx.x;
@@ -509,6 +521,19 @@ __device__ inline uint64_t reach(const LogitRow &row, const RowLimits &l, bool b
     }
 }
 
+// Among the row's tokens down to l.cut.
+__device__ inline uint64_t reach_in_row(const LogitRow &row, const RowLimits &l, bool by_weight, uint64_t target, ChooseShared &c)
+{
+    return reach([&](const auto &f) {
+#pragma unroll 1
+        for (uint32_t i = threadIdx.x; i < row.V; i += kSampleThreads) {
+            const float x = row[i];
+            const uint64_t place = place_of(x, i);
+            if (x != -INFINITY && place >= l.cut) f(place);
+        }
+    }, l, by_weight, target, 0, kPlaceBits, c);
+}
+
 // The token of a row by reading it as often as it takes; l.cut is 0.
 __device__ inline int32_t choose_anywhere(const LogitRow &row, const RowParams &q, RowLimits &l, ChooseShared &c)
 {
@@ -518,7 +543,7 @@ __device__ inline int32_t choose_anywhere(const LogitRow &row, const RowParams &
         uint64_t count = 0;
         for (uint32_t i = threadIdx.x; i < row.V; i += kSampleThreads) count += row[i] != -INFINITY;
         count = block_total(count, c);
-        if ((uint32_t)q.top_k < count) l.cut = reach(row, l, false, (uint32_t)q.top_k, c);
+        if ((uint32_t)q.top_k < count) l.cut = reach_in_row(row, l, false, (uint32_t)q.top_k, c);
     }
     if (q.top_p < 1.0f) {
         uint64_t total = 0;
@@ -527,7 +552,7 @@ __device__ inline int32_t choose_anywhere(const LogitRow &row, const RowParams &
             total += x != -INFINITY && place_of(x, i) >= l.cut ? l.units(l.weight(x)) : 0;
         }
         total = block_total(total, c);
-        l.cut = max(l.cut, reach(row, l, true, min(q.share((double)total), total), c));
+        l.cut = max(l.cut, reach_in_row(row, l, true, min(q.share((double)total), total), c));
     }
     return choose_by_runs(row, q, l, c);
 }
@@ -756,50 +781,72 @@ __device__ inline bool find_bin(const RowWork &work, const RowLimits &l, const S
 // Finds the last kept place (l.cut) in the bin in which top_p ends: reads the row for the bin's tokens; false if they are too many.
 __device__ inline bool cut_in_bin(const LogitRow &row, const RowParams &q, RowLimits &l, const LastBin &last, ChooseShared &c)
 {
+    constexpr uint32_t kAtOnce = 4;
     const uint32_t lane = threadIdx.x & 63, units = row.units();
     const BinScale scale(q.temperature);
     const float from = (float)last.bin, to = (float)(last.bin + 1);
     if (threadIdx.x == 0) c.listed = 0;
     __syncthreads();
 #pragma unroll 1
-    for (uint32_t unit = threadIdx.x; unit < units; unit += 2 * kSampleThreads) {
-        LogitRow::Raw raw[2];
-        raw[0] = row.raw(unit);
-        if (unit + kSampleThreads < units) raw[1] = row.raw(unit + kSampleThreads);
+    for (uint32_t unit = threadIdx.x; unit < units; unit += kAtOnce * kSampleThreads) {
+        LogitRow::Raw raw[kAtOnce];
 #pragma unroll
-        for (uint32_t k = 0; k < 2; ++k) {
+        for (uint32_t k = 0; k < kAtOnce; ++k)
+            if (unit + k * kSampleThreads < units) raw[k] = row.raw(unit + k * kSampleThreads);
+        float x[kAtOnce][8];
+        uint32_t marked = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
             if (unit + k * kSampleThreads >= units) break;
-            float x[8];
-            row.convert(raw[k], unit + k * kSampleThreads, x);
-            uint32_t marked = 0;
+            row.convert(raw[k], unit + k * kSampleThreads, x[k]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float y = scale.raw(x[i]);
-                marked |= (y >= from && y < to && x[i] != -INFINITY ? 1u : 0u) << i;
+                const float y = scale.raw(x[k][i]);
+                marked |= (y >= from && y < to && x[k][i] != -INFINITY ? 1u : 0u) << (8 * k + i);
             }
-            while (marked) {
-                const uint32_t i = __builtin_ctz(marked), index = (unit + k * kSampleThreads) * 8 + i, slot = atomicAdd(&c.listed, 1u);
-                marked &= marked - 1;
-                if (slot < kMostListed) c.places[slot] = place_of(row[index], index);
-            }
+        }
+        // one for all of a thread's: what waits costs more than what is counted
+        uint32_t slot = marked ? atomicAdd(&c.listed, (uint32_t)__popc(marked)) : 0;
+        while (marked) {
+            const uint32_t at = __builtin_ctz(marked);
+            float value = x[0][0];
+#pragma unroll
+            for (uint32_t j = 1; j < 8 * kAtOnce; ++j) value = at == j ? x[j / 8][j % 8] : value;
+            marked &= marked - 1;
+            if (slot < kMostListed) c.places[slot] = place_of(value, (unit + at / 8 * kSampleThreads) * 8 + at % 8);
+            ++slot;
         }
     }
     __syncthreads();
     const uint32_t count = c.listed;
     if (count > kMostListed) return false;
-    if (threadIdx.x < 64) {
-        RowLimits all = l;
-        all.min_p = 0;
-        const uint64_t weight = listed_weight(c.places, count, all);
-        if (weight != 0) {
-            const uint64_t cut = reach_listed(c.places, count, l, true, min(max((uint64_t)ceil(last.want), (uint64_t)1), weight), c);
-            if (lane == 0) c.prefix = cut;
-        }
-        if (lane == 0) c.single = weight != 0;
+    // the bin's weight, and what its places have in common
+    uint64_t weight = 0, most = 0, least = 0;
+    const auto each = [&](const auto &f) {
+#pragma unroll 1
+        for (uint32_t j = threadIdx.x; j < count; j += kSampleThreads) f(c.places[j]);
+    };
+    each([&](uint64_t place) {
+        most = max(most, place);
+        least = max(least, ~place);
+        weight += l.units(l.weight(logit_of(place)));
+    });
+    weight = block_total(weight, c);
+    if (weight == 0) return false;
+    most = wave_largest(most);
+    least = wave_largest(least);
+    if (threadIdx.x == 0) c.before = c.prefix = 0;
+    __syncthreads();
+    if (lane == 0) {
+        atomicMax((unsigned long long *)&c.before, (unsigned long long)most);
+        atomicMax((unsigned long long *)&c.prefix, (unsigned long long)least);
     }
     __syncthreads();
-    l.cut = c.prefix;
-    return c.single != 0;
+    most = c.before;
+    const uint32_t left = most == ~c.prefix ? 0 : 64 - __builtin_clzll(most ^ ~c.prefix);
+    __syncthreads();
+    l.cut = left == 0 ? most : reach(each, l, true, min(max((uint64_t)ceil(last.want), (uint64_t)1), weight), most >> left, left, c);
+    return true;
 }
 
 __device__ inline int32_t choose_row(const SampleProblem &p, uint32_t r, ChooseShared &c)
