@@ -868,14 +868,24 @@ __device__ inline int32_t choose_row(const SampleProblem &p, uint32_t r, ChooseS
         const uint32_t count = gather_lists(work, mine, c);
         if (count <= kMostListed) {
             const uint32_t down_to = wave_largest(lane < work.slices && mine.first ? mine.down_to : 0);
-            if (threadIdx.x < 64) {
-                const int32_t token = choose_listed(count, q, l, down_to, total, c);
-                if (lane == 0) c.token = token;
+            bool tell = true;
+            if (!q.top_k && !(q.min_p > 0.0f) && down_to > key_of(-INFINITY) + 1) {
+                // with top_p alone the lists tell if they weigh as much: all wavefronts add that faster than one finds that they do not
+                uint64_t weight = 0;
+#pragma unroll 1
+                for (uint32_t j = threadIdx.x; j < count; j += kSampleThreads) weight += c.places[j] >> 20 >= down_to ? l.units(l.weight(logit_of(c.places[j]))) : 0;
+                tell = q.share(total) <= block_total(weight, c);
             }
-            __syncthreads();
-            const int32_t token = c.token;
-            __syncthreads();
-            if (token >= 0) return token;
+            if (tell) {
+                if (threadIdx.x < 64) {
+                    const int32_t token = choose_listed(count, q, l, down_to, total, c);
+                    if (lane == 0) c.token = token;
+                }
+                __syncthreads();
+                const int32_t token = c.token;
+                __syncthreads();
+                if (token >= 0) return token;
+            }
         }
         LastBin last;
         const bool by_bin = !q.top_k && q.top_p < 1.0f && find_bin(work, l, mine, BinScale(q.temperature).of(l.top), (double)q.share(total), last, c) && cut_in_bin(row, q, l, last, c);
