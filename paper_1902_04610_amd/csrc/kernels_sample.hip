@@ -205,17 +205,31 @@ struct BinScale {
 };
 
 constexpr uint32_t kSliceLoads = kSlice / 8 / kSliceThreads;      // units of a thread
-// The sum of eight weights, and each: as Weights::of, but what is below 2^-64 counts as that.
+// As Weights::of, but what is below 2^-64 counts as that: 2^(n / 32) 2^f of a table and the series up to f^4 on [-1/64, 1/64], whose next term is below
+// (ln 2 / 64)^5 / 5! = 2e-12; 3 2^46 rounds to multiples of 1/32.
+constexpr uint32_t kPowers = 32;
 struct SliceWeights {
     double top, per, least;
-    __device__ SliceWeights(float t, float temperature) : top(t), per(1.4426950408889634 / (double)temperature), least(-64.0 / per) {}
-    __device__ double of(float x) const { return power_of_two(fmax((double)x - top, least), per); }
+    const double *powers;
+    __device__ SliceWeights(float t, float temperature, const double *table) : top(t), per(1.4426950408889634 / (double)temperature), least(-64.0 / per), powers(table) {}
+    __device__ static double power(uint32_t i) { return 2.0 * power_of_two((double)i - kPowers, 1.0 / kPowers); }
+    __device__ double of(float x) const
+    {
+        constexpr double kWhole = 211106232532992.0, kLn2 = 0.6931471805599453, k2 = kLn2 * kLn2;
+        const double d = fmax((double)x - top, least), whole = fma(d, per, kWhole), f = fma(d, per, kWhole - whole);
+        const int32_t n = (int32_t)(uint32_t)__builtin_bit_cast(uint64_t, whole);
+        double v = fma(k2 * k2 / 24, f, k2 * kLn2 / 6);
+        v = fma(v, f, k2 / 2);
+        v = fma(v, f, kLn2);
+        v = fma(v, f, 1.0) * powers[n & (int32_t)(kPowers - 1)];
+        return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, v) + ((uint64_t)(uint32_t)(n >> 5) << 52));
+    }
 };
 
 struct SliceShared {
     f32x4 x[2 * kSliceLoads * kSliceThreads];      // a thread's j-th unit: four logits at 2 j kSliceThreads + its number, four kSliceThreads further
     uint32_t keys[kSliceThreads], counts[kSliceWaves], firsts[kSliceWaves], down_to;
-    double masses[kSliceWaves];
+    double masses[kSliceWaves], powers[kPowers];
     unsigned long long bins[kMassBins];
 };
 
@@ -251,6 +265,7 @@ __device__ inline void slice_row(const SampleProblem &p, uint32_t r, uint32_t sl
     const bool binned = massed && q.top_p < 1.0f && scale.usable();
     if (binned)
         for (uint32_t i = threadIdx.x; i < kMassBins; i += kSliceThreads) s.bins[i] = 0;
+    if (massed && threadIdx.x < kPowers) s.powers[threadIdx.x] = SliceWeights::power(threadIdx.x);
     __syncthreads();
     // every wavefront has all of them
     const u32x4 key0 = *(const u32x4 *)&s.keys[4 * lane], key1 = *(const u32x4 *)&s.keys[256 + 4 * lane];
@@ -289,7 +304,7 @@ __device__ inline void slice_row(const SampleProblem &p, uint32_t r, uint32_t sl
     const float low = listed ? float_of(s.down_to) : INFINITY;
     const bool has_top = __any(mine == top);
     const int32_t top_bin = scale.of(top);
-    const SliceWeights weights(top, q.temperature);
+    const SliceWeights weights(top, q.temperature, s.powers);
     Global<uint64_t> *list = work.list(slice, wave);
     uint32_t first = ~0u, count = 0;
     double mass = 0;
