@@ -19,7 +19,10 @@ constexpr int32_t kStride = 4 * (int32_t)kKeys;      // keys between two tiles o
 // Few rows, one sequence of 8 key heads of 128, us for 500 / 1000 / 4000 / 16000 keys: parts of 256 10.6 11.1 11.4 19.9, of 512 8.4 12.3 12.6 18.9, of 1024 8.4
 // 10.8 16.5 19.5: up to kWhole keys a second launch costs more than it saves.  16 such sequences, 1000 / 2000 keys: 18.5 28.9, 20.7 28.5, 16.2 32.6; 16 jobs,
 // 136 sequences of 1 .. 6000 keys: 80, 67, 63.  The rule knows the job alone, not the call's others: what a job is answered does not depend on its neighbours.
-constexpr uint32_t kWhole = 1024, kLeastPart = 512, kTarget = 512;
+// Prompts and chunks: a workgroup fills a compute unit, and what the rule cannot know (rows are a bound, jobs are several) makes more than one round of them likely.
+// us with 512 / 256 / 192 workgroups wanted: chunks of 512 behind 8000 .. 20000 keys, a window of 4096, 102 96 78; of 512 behind 8000 120 96 107; a prompt of 2048 92 64
+// 63; 256 behind 16000 58 75 81; 11 such shapes 0.91 and 0.88 of the time of 512.
+constexpr uint32_t kWhole = 1024, kLeastPart = 512, kFewTarget = 512, kManyTarget = 192;
 
 AttentionParts attention_parts(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len, uint32_t window)
 {
@@ -28,7 +31,9 @@ AttentionParts attention_parts(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_
     const uint32_t columns = many ? many_columns(D) : kFewColumns;
     const uint64_t tiles = (uint64_t)ColumnBase{G, columns}(M, n_seqs) * Hkv;
     const auto part = [&](uint64_t keys) {
-        return keys <= kWhole ? kWhole : std::max<uint64_t>(kLeastPart, (keys * std::min<uint64_t>(tiles, kTarget) / kTarget + 127) / 128 * 128);
+        if (keys <= kWhole) return (uint64_t)kWhole;
+        const uint64_t target = many ? kManyTarget : kFewTarget, about = std::max<uint64_t>(kLeastPart, keys * std::min(tiles, target) / target), n = (keys + about - 1) / about;
+        return ((keys + n - 1) / n + 127) / 128 * 128;
     };
     const auto parts = [](uint64_t keys, uint64_t of) { return (keys + of - 1) / of; };
     const uint64_t most = parts(max_len, part(max_len));      // what there is room for
