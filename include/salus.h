@@ -502,7 +502,7 @@ int32_t salus_grouped_attention(salus_pool_t *pool, const salus_attention_desc *
  *     the first top_k (0 and below: all),  of these the fewest from the front whose w reach top_p of their sum,  of these those with w >= min_p,
  * at least the first, and the token is the smallest index up to which the sum of the kept w, in order of index, exceeds u times the sum of all kept.  Temperature 0 and below (or NaN): the first
  * of the order.  top_p of 1 and above or NaN, min_p of 0 and below or NaN: no limit; u is cut to [0, 1).  A NaN counts as minus infinity; where nothing is larger, the token is -1.
- * Weights are in 64 bits and count in steps of 2^-44 of the largest, whose sums do not depend on any order.  tokens: M int32, written. work:
+ * Weights are in 64 bits, to 1e-11 of themselves or 2^-44 of the largest, and summed in an order that does not change: the same call gives the same tokens.  tokens: M int32, written. work:
  * salus_sample_work_bytes().  V is at least 1 and at most 2^19. */
 typedef struct {
     int32_t  job;

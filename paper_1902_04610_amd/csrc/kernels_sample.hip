@@ -7,18 +7,20 @@
 // Every limit keeps a beginning of the order, so nothing is sorted: the place of a token in the order is a 52-bit number (the logit's bits, made
 // monotonous, in front of the index), and a limit is the number of the last token that is kept.
 //
-// Bound by reading the logits, once.  Two kernels:
+// Two kernels.  Reading the logits once would take 9 us for 256 rows of 128256 bf16; this takes 86 with rows of all kinds of limits (16 for one row of 32000 floats):
 //   slice_rows    a workgroup takes 8192 logits of a row and leaves their first token, their sum of weights if the row wants it, and the places of
 //                 those that a limit may keep, in order of index: all down to a threshold that at least so many of its threads' largest logits reach as
-//                 the limit may want of one slice; for top_p also the weight in bins of 1 / 16 of a power of two.
-//   choose_rows   a workgroup per row puts that together.  Without limits it reads one slice again; where the kept tokens all lie above every
-//                 slice's threshold, which the lists tell, none.  Else it finds the bin in which top_p ends, reads the row once for the kept weight of sixteen
-//                 runs of it and for that bin's tokens, and one run again for the token.
+//                 the limit may want of one slice; for top_p also the weight in bins of 1 / 16 of a power of two.  Bound by its vector instructions: 18 us
+//                 for greedy rows, 27 with lists, 40 with 64-bit weights, 56 with bins.
+//   choose_rows   a workgroup per row puts that together.  Without limits it reads one slice again (10 us); where the kept tokens all lie above every
+//                 slice's threshold, which the lists tell, none (8 - 20).  Else it finds the bin in which top_p ends, reads the row once for that bin's tokens, and one
+//                 slice again for the token (45 for one such row: one compute unit's latencies and instructions, a chain of some ten barriers); with min_p too it
+//                 reads the row again for the kept weight of sixteen runs.
 // What even that does not hold (lists that run over: thousands of equal logits, top_k beyond them) is found by reading the row several times
 // (choose_anywhere), eleven bits of the last place at a time by histograms of how many tokens there are, or how much weight.
 //
-// Weights are 64-bit exponentials of differences to the row's largest logit; where they are summed by atomic additions they count as whole multiples of 2^-44, so that
-// no order shows.
+// Weights are 64-bit exponentials of differences to the row's largest logit, to 1e-11; where they are summed by atomic additions they count as whole multiples of 2^-44, so
+// that no order shows.
 #include <cfloat>
 
 #include "answer.hpp"
@@ -388,7 +390,7 @@ __global__ __launch_bounds__(kSliceThreads, 8) void slice_rows(Args a)
 }
 
 // The code of this kernel runs once a row: what is not kept short is waited for line by line, so that loops are not unrolled and paths share their pieces.
-constexpr uint32_t kPieceSums = 32;      // of a wavefront: a piece of a row has at most 2^19 / 16 tokens
+constexpr uint32_t kPieceSums = 4;       // of a wavefront, 512 tokens each: a piece of a row has at most 2^19 / 16
 struct ChooseShared {
     unsigned long long mass[kBins];
     uint32_t count[kBins];
@@ -412,48 +414,51 @@ __device__ inline Piece choose_piece(const RowParams &q, double mass)
     return {at, target - (at ? lane_value(all, at - 1) : 0.0)};
 }
 
-// The token among logits from .. to of a row, `left` (of the largest weight) in front of it there; `first` if nothing there weighs half a unit.
+// The token among logits from .. to of a row (from a multiple of eight), `left` (of the largest weight) in front of it there; `first` if nothing there weighs half a unit.
 __device__ inline int32_t choose_in(const LogitRow &row, const RowLimits &l, uint32_t from, uint32_t to, double left, uint32_t first, ChooseShared &c)
 {
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, end = (to + 7) / 8;
+    const auto eight = [&](uint32_t unit, uint64_t (&w)[8]) {
+        uint64_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = 0;
+        if (unit < end) {
+            float x[8];
+            row.convert(row.raw(unit), unit, x);
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) sum += w[i] = l.kept(x[i], unit * 8 + i);
+        }
+        return sum;
+    };
     __syncthreads();
+    uint64_t w[8];
     uint32_t n = 0;
 #pragma unroll 1
-    for (uint32_t at = from; at < to; at += 8 * kSampleThreads) {
-        float x[8];
-#pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) {
-            const uint32_t i = at + k * kSampleThreads + threadIdx.x;
-            x[k] = i < to ? row[i] : -INFINITY;
-        }
-#pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) {
-            if (at + k * kSampleThreads >= to) break;
-            const uint64_t sum = wave_total(l.kept(x[k], at + k * kSampleThreads + threadIdx.x));
-            if (lane == 0) c.sums[n * kSampleWaves + wave] = sum;
-            ++n;
-        }
+    for (uint32_t at = from / 8; at < end; at += kSampleThreads, ++n) {
+        const uint64_t sum = wave_total(eight(at + threadIdx.x, w));
+        if (lane == 0) c.sums[n * kSampleWaves + wave] = sum;
     }
     if (threadIdx.x == 0) c.token = (int32_t)first;
     __syncthreads();
-    // runs of sums: one wavefront finds whose token it is, and the token
-    n *= kSampleWaves;
-    constexpr uint32_t kEach = kPieceSums * kSampleWaves / 64;
+    // sums of 64 units each: one wavefront finds whose token it is, and the token
+    static_assert(kPieceSums * kSampleWaves == 64, "one a lane");
     if (wave == 0) {
-        uint64_t mine = 0;
-        for (uint32_t i = 0; i < kEach; ++i) mine += kEach * lane + i < n ? c.sums[kEach * lane + i] : 0;
-        const uint64_t scan = wave_sum_scan(mine), all = lane_value(scan, 63);
+        const uint64_t mine = lane < n * kSampleWaves ? c.sums[lane] : 0, scan = wave_sum_scan(mine), all = lane_value(scan, 63);
         if (all != 0) {
             // (the sums of pieces are rounded otherwise: the last token that weighs anything if none passes)
             const uint64_t want = min((uint64_t)(fmax(left, 0.0) * kWeightUnit), all - 1);
-            const uint32_t owner = __builtin_ctzll(__ballot(scan > want));
-            uint64_t before = lane_value(scan - mine, owner);
-            uint32_t run = kEach * owner;
-            while (before + c.sums[run] <= want) before += c.sums[run++];
-            const uint32_t i = from + run * 64 + lane;
-            const uint64_t w = i < to ? l.kept(row[i], i) : 0;
-            const uint64_t past = __ballot(before + wave_sum_scan(w) > want);
-            if (lane == 0) c.token = (int32_t)(from + run * 64 + __builtin_ctzll(past));
+            const uint32_t owner = __builtin_ctzll(__ballot(scan > want)), unit = from / 8 + 64 * owner + lane;
+            const uint64_t sum = eight(unit, w), up_to = lane_value(scan - mine, owner) + wave_sum_scan(sum);
+            uint64_t before = up_to - sum;
+            if (before <= want && want < up_to) {
+                uint32_t at = 0;
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) {
+                    if (before <= want) at = i;
+                    before += w[i];
+                }
+                c.token = (int32_t)(unit * 8 + at);
+            }
         }
     }
     __syncthreads();
@@ -597,143 +602,92 @@ __device__ inline uint32_t gather_lists(const RowWork &work, const Slice &mine, 
     __syncthreads();
     static_assert(kListed == 64 && kSliceWaves * 64 <= 1024, "one a lane");
     const Global<uint64_t> *lists = work.list(0, 0);
-#pragma unroll 4
-    for (uint32_t i = wave; i < work.slices * kSliceWaves; i += kSampleWaves) {
-        const uint32_t to = c.count[i] + lane;
-        if (to < c.count[1024 + i]) c.places[to] = lists[i * kListed + lane];
+    // eight lists of a wavefront at once; what stands behind a list's end is read and dropped
+#pragma unroll 1
+    for (uint32_t i0 = wave; i0 < work.slices * kSliceWaves; i0 += 8 * kSampleWaves) {
+        uint64_t place[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) place[k] = lists[min(i0 + k * kSampleWaves, work.slices * kSliceWaves - 1) * kListed + lane];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) {
+            const uint32_t i = i0 + k * kSampleWaves;
+            if (i >= work.slices * kSliceWaves) break;
+            const uint32_t to = c.count[i] + lane;
+            if (to < c.count[1024 + i]) c.places[to] = place[k];
+        }
     }
     __syncthreads();
     return all;
 }
 
-// What follows is one wavefront's: the lists are short, and barriers of sixteen wavefronts would take longer than what lies between them.
-
-// As reach(), among places[0 .. count); 256 bins at a time of the range that the places take.
-__device__ inline uint64_t reach_listed(const uint64_t *places, uint32_t count, const RowLimits &l, bool by_weight, uint64_t target, ChooseShared &c)
-{
-    const uint32_t lane = threadIdx.x & 63;
-    uint64_t from = ~0ull, span = 0;             // the token is among from .. from + span - 1
-    for (uint32_t i = lane; i < count; i += 64) {
-        from = min(from, places[i]);
-        span = max(span, places[i]);
-    }
-    from = ~wave_largest(~from);
-    span = wave_largest(span) - from + 1;
-#pragma unroll 1
-    for (;;) {
-        const uint32_t bits = 64 - __builtin_clzll(span - 1 | 1), shift = bits > 8 ? bits - 8 : 0;
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-            c.count[4 * lane + i] = 0;
-            c.mass[4 * lane + i] = 0;
-        }
-        wave_sync();
-#pragma unroll 1
-        for (uint32_t i = lane; i < count; i += 64) {
-            const uint64_t place = places[i], off = place - from;
-            if (place < from || off >= span) continue;
-            const uint32_t bin = 255 - (uint32_t)(off >> shift);
-            atomicAdd(&c.count[bin], 1u);
-            if (by_weight) atomicAdd(&c.mass[bin], (unsigned long long)l.units(l.weight(logit_of(place))));
-        }
-        wave_sync();
-        // four bins a lane, the earliest tokens in front
-        uint64_t n[4], sum = 0;
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) sum += n[i] = by_weight ? c.mass[4 * lane + i] : c.count[4 * lane + i];
-        const uint64_t scan = wave_sum_scan(sum);
-        uint64_t before = scan - sum;
-        const uint32_t owner = __builtin_ctzll(__ballot(scan >= target) | 1ull << 63);
-        uint32_t bin = 4 * lane;
-        uint64_t in_front = before;
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-            if (before < target && target <= before + n[i]) {
-                bin = 4 * lane + i;
-                in_front = before;
-            }
-            before += n[i];
-        }
-        bin = lane_value(bin, owner);
-        target -= lane_value(in_front, owner);
-        from += (uint64_t)(255 - bin) << shift;
-        span = 1ull << shift;
-        const bool single = c.count[bin] == 1;
-        wave_sync();
-        if (shift == 0 || single) return from;
-    }
-}
-
-// Leaves of places[0 .. count) those down to `cut`, in order; how many.
-__device__ inline uint32_t keep_from(uint64_t *places, uint32_t count, uint64_t cut)
-{
-    const uint32_t lane = threadIdx.x & 63;
-    uint32_t n = 0;
-#pragma unroll 1
-    for (uint32_t at = 0; at < count; at += 64) {
-        const uint64_t place = at + lane < count ? places[at + lane] : 0;
-        const bool kept = at + lane < count && place >= cut;
-        const uint64_t all = __ballot(kept);
-        wave_sync();
-        if (kept) places[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] = place;
-        n += __popcll(all);
-    }
-    wave_sync();
-    return n;
-}
-
-__device__ inline uint64_t listed_weight(const uint64_t *places, uint32_t count, const RowLimits &l)
-{
-    uint64_t sum = 0;
-#pragma unroll 1
-    for (uint32_t i = threadIdx.x & 63; i < count; i += 64) sum += l.kept(logit_of(places[i]), index_of(places[i]));
-    return wave_total(sum);
-}
-
 // The token of a row whose lists have what its limits may keep: known down to `down_to` (the upper bits of a place).  total: the row's weight, if it is known.  -1 if the lists
-// do not tell.
+// do not tell.  (One wavefront alone, without barriers, is quicker below some 200 places and takes 20 us for 1500, this 5.)
 __device__ inline int32_t choose_listed(uint32_t count, const RowParams &q, RowLimits l, uint32_t down_to, double total, ChooseShared &c)
 {
-    const uint32_t lane = threadIdx.x & 63;
+    static_assert(kMostListed == 4 * kSampleThreads, "four places a thread");
     const double min_p = l.min_p;
     l.min_p = 0;             // (for the sums)
     // everything there is is known, or everything that min_p keeps
     const bool everything = down_to <= key_of(-INFINITY) + 1;
     bool known = everything || (min_p > 0.0 && l.weight(float_of(down_to)) < min_p);
     uint64_t cut = (uint64_t)down_to << 20;
-    // by the threshold, by top_k, by top_p
+    const auto each = [&](const auto &f) {
 #pragma unroll 1
-    for (int limit = 0;; ++limit) {
-        count = keep_from(c.places, count, cut);
-        bool by_weight = false;
-        uint64_t target;
-        if (limit == 0 && q.top_k) {
-            if (count >= (uint32_t)q.top_k) known = true;
-            else if (!everything && q.top_p < 1.0f) return -1;         // the sum of what top_k keeps is not known
-            if (count <= (uint32_t)q.top_k) continue;
-            target = (uint32_t)q.top_k;
-        } else if (limit <= 1 && q.top_p < 1.0f) {
-            const uint64_t weight = listed_weight(c.places, count, l);
-            const bool all = everything || q.top_k;      // these are all that share the weight
-            target = all ? min(q.share((double)weight), weight) : q.share(total);
-            by_weight = true;
-            limit = 1;
-            if (target > weight) break;
+        for (uint32_t j = threadIdx.x; j < count; j += kSampleThreads)
+            if (c.places[j] >= cut) f(c.places[j]);
+    };
+    // what lies between `cut` and the first token
+    const auto reach_from_cut = [&](bool by_weight, uint64_t target) {
+        const uint32_t left = l.first == cut ? 0 : 64 - __builtin_clzll(l.first ^ cut);
+        if (left != 0) cut = reach(each, l, by_weight, target, l.first >> left, left, c);
+    };
+    if (q.top_k) {
+        uint64_t n = 0;
+        each([&](uint64_t) { ++n; });
+        n = block_total(n, c);
+        if (n >= (uint32_t)q.top_k) known = true;
+        else if (!everything && q.top_p < 1.0f) return -1;         // the sum of what top_k keeps is not known
+        if (n > (uint32_t)q.top_k) reach_from_cut(false, (uint32_t)q.top_k);
+    }
+    if (q.top_p < 1.0f) {
+        uint64_t weight = 0;
+        each([&](uint64_t place) { weight += l.units(l.weight(logit_of(place))); });
+        weight = block_total(weight, c);
+        const bool all = everything || q.top_k;      // these are all that share the weight
+        const uint64_t target = all ? min(q.share((double)weight), weight) : q.share(total);
+        if (target <= weight) {
             known = true;
-        } else break;
-        cut = reach_listed(c.places, count, l, by_weight, target, c);
+            reach_from_cut(true, target);
+        }
     }
     if (!known) return -1;
     l.min_p = min_p;
-    const uint64_t all = listed_weight(c.places, count, l), want = min((uint64_t)q.before((double)all), all - 1);      // (the product may be rounded up)
-    uint64_t before = 0;
-#pragma unroll 1
-    for (uint32_t at = 0;; at += 64) {
-        const uint64_t w = at + lane < count ? l.kept(logit_of(c.places[at + lane]), index_of(c.places[at + lane])) : 0, scan = before + wave_sum_scan(w);
-        const uint64_t past = __ballot(scan > want);
-        if (past) return (int32_t)index_of(c.places[at + __builtin_ctzll(past)]);
-        before = lane_value(scan, 63);
+    uint64_t w[4], sum = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) {
+        const uint32_t j = 4 * threadIdx.x + k;
+        const uint64_t place = j < count ? c.places[j] : 0;
+        w[k] = j < count && place >= cut ? l.kept(logit_of(place), index_of(place)) : 0;
+        sum += w[k];
     }
+    const uint64_t scan = wave_sum_scan(sum);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) c.part[threadIdx.x >> 6] = scan;
+    __syncthreads();
+    uint64_t before = scan - sum, all = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kSampleWaves; ++i) {
+        before += i < threadIdx.x >> 6 ? c.part[i] : 0;
+        all += c.part[i];
+    }
+    const uint64_t want = min((uint64_t)q.before((double)all), all - 1);      // (the product may be rounded up)
+    if (before <= want && want < before + sum) {
+        uint32_t k = 0;
+        while (k < 3 && before + w[k] <= want) before += w[k++];
+        c.token = (int32_t)index_of(c.places[4 * threadIdx.x + k]);
+    }
+    __syncthreads();
+    return c.token;
 }
 
 // The bin in which the row's weight reaches `share` units (lane i: slice i), by all slices' bins, and how much of it that takes; false if it is none of theirs.
@@ -798,8 +752,20 @@ __device__ inline bool cut_in_bin(const LogitRow &row, const RowParams &q, RowLi
 {
     constexpr uint32_t kAtOnce = 4;
     const uint32_t lane = threadIdx.x & 63, units = row.units();
+    // the bin's logits: bins do not fall as logits grow, so a search among the floats' numbers finds its smallest and the next bin's
     const BinScale scale(q.temperature);
-    const float from = (float)last.bin, to = (float)(last.bin + 1);
+    const auto first_of = [&](int32_t bin) {
+        uint32_t low = key_of(-INFINITY), high = key_of(INFINITY);       // the bin of `low` is smaller; `high` is that of infinity
+#pragma unroll 1
+        while (high - low > 1) {
+            const uint32_t step = (high - low + 63) / 64, at = min(low + (lane + 1) * step, high);
+            const uint32_t reached = __builtin_ctzll(__ballot(at == high || scale.of(float_of(at)) >= bin));
+            high = min(low + (reached + 1) * step, high);
+            low += reached * step;
+        }
+        return float_of(high);
+    };
+    const float from = first_of(last.bin), to = first_of(last.bin + 1);
     if (threadIdx.x == 0) c.listed = 0;
     __syncthreads();
 #pragma unroll 1
@@ -815,10 +781,7 @@ __device__ inline bool cut_in_bin(const LogitRow &row, const RowParams &q, RowLi
             if (unit + k * kSampleThreads >= units) break;
             row.convert(raw[k], unit + k * kSampleThreads, x[k]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float y = scale.raw(x[k][i]);
-                marked |= (y >= from && y < to && x[k][i] != -INFINITY ? 1u : 0u) << (8 * k + i);
-            }
+            for (int i = 0; i < 8; ++i) marked |= (x[k][i] >= from && x[k][i] < to ? 1u : 0u) << (8 * k + i);
         }
         // one for all of a thread's: what waits costs more than what is counted
         uint32_t slot = marked ? atomicAdd(&c.listed, (uint32_t)__popc(marked)) : 0;
@@ -883,24 +846,8 @@ __device__ inline int32_t choose_row(const SampleProblem &p, uint32_t r, ChooseS
         const uint32_t count = gather_lists(work, mine, c);
         if (count <= kMostListed) {
             const uint32_t down_to = wave_largest(lane < work.slices && mine.first ? mine.down_to : 0);
-            bool tell = true;
-            if (!q.top_k && !(q.min_p > 0.0f) && down_to > key_of(-INFINITY) + 1) {
-                // with top_p alone the lists tell if they weigh as much: all wavefronts add that faster than one finds that they do not
-                uint64_t weight = 0;
-#pragma unroll 1
-                for (uint32_t j = threadIdx.x; j < count; j += kSampleThreads) weight += c.places[j] >> 20 >= down_to ? l.units(l.weight(logit_of(c.places[j]))) : 0;
-                tell = q.share(total) <= block_total(weight, c);
-            }
-            if (tell) {
-                if (threadIdx.x < 64) {
-                    const int32_t token = choose_listed(count, q, l, down_to, total, c);
-                    if (lane == 0) c.token = token;
-                }
-                __syncthreads();
-                const int32_t token = c.token;
-                __syncthreads();
-                if (token >= 0) return token;
-            }
+            const int32_t token = choose_listed(count, q, l, down_to, total, c);
+            if (token >= 0) return token;
         }
         LastBin last;
         const bool by_bin = !q.top_k && q.top_p < 1.0f && find_bin(work, l, mine, BinScale(q.temperature).of(l.top), (double)q.share(total), last, c) && cut_in_bin(row, q, l, last, c);

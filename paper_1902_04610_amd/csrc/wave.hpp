@@ -38,14 +38,6 @@ __device__ inline int wave_find_range(uint64_t excl, uint64_t x, bool valid)
     return 63 - __clzll((long long)m);
 }
 
-// What the lanes of a wavefront wrote to LDS in front of this is what they read behind it (they run in step: nothing waits, the compiler keeps the order).
-__device__ inline void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // Sums and maxima across the lanes by data-parallel moves (row shifts by 1, 2, 4, 8, then the last lane of a row, or of two, to the rows behind it): some ten cycles a step, where
 // a shuffle takes a hundred.  T: any type of 4 or 8 bytes whose zero is all bits zero; lanes without a source get zero.
 template <int CONTROL, int ROWS, typename T>
