@@ -469,7 +469,7 @@ __device__ inline int32_t choose_in(const LogitRow &row, const RowLimits &l, uin
 __device__ inline int32_t choose_by_runs(const LogitRow &row, const RowParams &q, const RowLimits &l, ChooseShared &c)
 {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, run = (row.V + kSampleThreads - 1) / kSampleThreads * 64;
-    const uint32_t from = min(wave * run, row.V), to = min(from + run, row.V);
+    const uint32_t from = wave * run, to = min(from + run, row.V);        // (the last ones may begin behind the row)
     uint64_t sum = 0;
 #pragma unroll 1
     for (uint32_t unit = from / 8 + lane; unit < (to + 7) / 8; unit += 64) {
@@ -498,7 +498,7 @@ __device__ inline uint64_t block_total(uint64_t v, ChooseShared &c)
 }
 
 // The place of the token with which the first ones of an order reach `target`, tokens or weight, among those whose places begin with `prefix` in front of the last
-// `left` bits.  each(f) calls f for each of a thread's tokens.
+// `left` bits.  each(f) calls f for each of a thread's tokens.  What it gives is at most that place, and above that of the next token of these.
 template <typename Each>
 __device__ inline uint64_t reach(const Each &each, const RowLimits &l, bool by_weight, uint64_t target, uint64_t prefix, uint32_t left, ChooseShared &c)
 {
@@ -639,7 +639,7 @@ __device__ inline int32_t choose_listed(uint32_t count, const RowParams &q, RowL
     // what lies between `cut` and the first token
     const auto reach_from_cut = [&](bool by_weight, uint64_t target) {
         const uint32_t left = l.first == cut ? 0 : 64 - __builtin_clzll(l.first ^ cut);
-        if (left != 0) cut = reach(each, l, by_weight, target, l.first >> left, left, c);
+        cut = left == 0 ? cut : max(cut, reach(each, l, by_weight, target, l.first >> left, left, c));
     };
     if (q.top_k) {
         uint64_t n = 0;
@@ -821,9 +821,11 @@ __device__ inline bool cut_in_bin(const LogitRow &row, const RowParams &q, RowLi
     }
     __syncthreads();
     most = c.before;
-    const uint32_t left = most == ~c.prefix ? 0 : 64 - __builtin_clzll(most ^ ~c.prefix);
+    const uint64_t smallest = ~c.prefix;
+    const uint32_t left = most == smallest ? 0 : 64 - __builtin_clzll(most ^ smallest);
     __syncthreads();
-    l.cut = left == 0 ? most : reach(each, l, true, min(max((uint64_t)ceil(last.want), (uint64_t)1), weight), most >> left, left, c);
+    // (not below the bin: what lies there is none of `each`)
+    l.cut = left == 0 ? most : max(smallest, reach(each, l, true, min(max((uint64_t)ceil(last.want), (uint64_t)1), weight), most >> left, left, c));
     return true;
 }
 

@@ -57,6 +57,43 @@ def test_all_limits(V, kind, bf16):
     run([sample_job(to_bf16(x) if bf16 else x, limits(rng, M), rng.uniform(0.0001, 0.9999, M), bf16, pad=8 * (V % 3))])
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("V", [1100, 2597, 3100, 4099, 8200])
+def test_rows_that_fill_only_some_of_their_runs(V, bf16):
+    """Flat rows whose kept tokens no list holds; random numbers up to the last of them."""
+    rng = np.random.default_rng(V)
+    x = (rng.standard_normal((64, V)) * 1.5).astype(np.float32)
+    limits = [(1.0, 0, 1.0, 0.01), (1.1, 0, 0.95, 0.01), (1.0, 600, 0.9, 0.0), (0.9, 500, 1.0, 0.02)]
+    run([sample_job(to_bf16(x) if bf16 else x, limits * 16, (np.arange(64) // 4 + 0.99) / 16, bf16)])
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("V", [900, 2597, 20011])
+def test_where_top_p_ends(V, bf16):
+    """One row after the other, behind top_k and alone: the last kept token and the first that is not differ by any of a place's bits."""
+    rng = np.random.default_rng(V)
+    x = (rng.standard_normal((96, V)) * 1.5).astype(np.float32)
+    limits = [(float(rng.uniform(0.6, 1.2)), 0 if i % 2 else int(rng.integers(20, 200)), float(rng.uniform(0.5, 0.97)), 0.0) for i in range(96)]
+    run([sample_job(to_bf16(x) if bf16 else x, limits, rng.choice([0.2, 0.5, 0.9, 0.97, 0.995, 0.9999], 96), bf16)])
+
+
+def test_top_p_ends_in_front_of_thousands_of_almost_equal_logits():
+    """Three kept tokens, the last a few float steps above 3000 equal ones, next to multiples of 1 / 16 of a power of two."""
+    rng = np.random.default_rng(3)
+    rows, limits, V = [], [], 3100
+    for n in range(30, 70):
+        edge = np.float32(n) / (np.float32(16.0) * np.float32(1.4426950))
+        step = np.spacing(edge)
+        x = np.full(V, -20.0, np.float32)
+        x[rng.permutation(V)[:3003]] = edge - 2 * step
+        three = rng.permutation(np.nonzero(x > 0)[0])[:3]
+        x[three] = edge + np.float32(1.5), edge + np.float32(0.02), edge + 4 * step
+        w = np.exp(x.astype(np.float64) - x.max())
+        rows.append(x)
+        limits.append((1.0, 0, float((w[three[:2]].sum() + 0.5 * w[three[2]]) / w.sum()), 0.0))
+    run([sample_job(np.array(rows), limits, rng.uniform(0.02, 0.98, len(rows)))])
+
+
 @pytest.mark.parametrize("V,M", [(131072, 3), (200003, 2), (524288, 1)])
 def test_large_vocabularies(V, M):
     rng = np.random.default_rng(V)
