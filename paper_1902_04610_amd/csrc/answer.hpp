@@ -52,7 +52,7 @@ struct SampleProblem {
 uint64_t sample_work_bytes(uint32_t M, uint32_t V);
 hipError_t launch_sample(const SampleProblem *p, uint32_t n, hipStream_t stream, uint64_t *launches);
 
-// Launches by value of at most 32 problems, or of at most 4 for rounds whose time is the host's.
+// Launches by value of at most 24 problems, or of at most 4 for rounds whose time is the host's.
 template <typename P, uint32_t NP>
 struct AnswerArgs {
     uint32_t n, tiles, base, pad;
