@@ -92,15 +92,21 @@ struct LogitRow {
         if (!bf16) r.w[1] = *(const Global<u32x4> *)(at + (uint64_t)unit * 32 + 16);
         return r;
     }
-    __device__ void convert(const Raw &r, uint32_t unit, float (&x)[8]) const
+    __device__ void values(const Raw &r, float (&x)[8]) const      // as they stand there
     {
         if (bf16) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = clean(i % 2 ? bf16_high(r.w[0][i / 2]) : bf16_low(r.w[0][i / 2]));
+            for (int i = 0; i < 8; ++i) x[i] = i % 2 ? bf16_high(r.w[0][i / 2]) : bf16_low(r.w[0][i / 2]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = clean(as_float(r.w[i / 4][i % 4]));
+            for (int i = 0; i < 8; ++i) x[i] = as_float(r.w[i / 4][i % 4]);
         }
+    }
+    __device__ void convert(const Raw &r, uint32_t unit, float (&x)[8]) const
+    {
+        values(r, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = clean(x[i]);
         if (unit * 8 + 8 > V) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = unit * 8 + i < V ? x[i] : -INFINITY;
@@ -763,9 +769,11 @@ __device__ inline bool cut_in_bin(const LogitRow &row, const RowParams &q, RowLi
             high = min(low + (reached + 1) * step, high);
             low += reached * step;
         }
-        return float_of(high);
+        return high;
     };
-    const float from = first_of(last.bin), to = first_of(last.bin + 1);
+    const uint32_t low = first_of(last.bin), high = first_of(last.bin + 1);
+    if (low >= high) return false;
+    const float from = float_of(low), to = float_of(high - 1);
     if (threadIdx.x == 0) c.listed = 0;
     __syncthreads();
 #pragma unroll 1
@@ -779,9 +787,12 @@ __device__ inline bool cut_in_bin(const LogitRow &row, const RowParams &q, RowLi
 #pragma unroll
         for (uint32_t k = 0; k < kAtOnce; ++k) {
             if (unit + k * kSampleThreads >= units) break;
-            row.convert(raw[k], unit + k * kSampleThreads, x[k]);
+            row.values(raw[k], x[k]);
+            uint32_t among = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) marked |= (x[k][i] >= from && x[k][i] < to ? 1u : 0u) << (8 * k + i);
+            for (int i = 0; i < 8; ++i) among |= (__builtin_amdgcn_fmed3f(x[k][i], from, to) == x[k][i] ? 1u : 0u) << i;      // (no NaN is)
+            if ((unit + k * kSampleThreads) * 8 + 8 > row.V) among &= (1u << row.V % 8) - 1;
+            marked |= among << (8 * k);
         }
         // one for all of a thread's: what waits costs more than what is counted
         uint32_t slot = marked ? atomicAdd(&c.listed, (uint32_t)__popc(marked)) : 0;
@@ -791,7 +802,7 @@ __device__ inline bool cut_in_bin(const LogitRow &row, const RowParams &q, RowLi
 #pragma unroll
             for (uint32_t j = 1; j < 8 * kAtOnce; ++j) value = at == j ? x[j / 8][j % 8] : value;
             marked &= marked - 1;
-            if (slot < kMostListed) c.places[slot] = place_of(value, (unit + at / 8 * kSampleThreads) * 8 + at % 8);
+            if (slot < kMostListed) c.places[slot] = place_of(LogitRow::clean(value), (unit + at / 8 * kSampleThreads) * 8 + at % 8);
             ++slot;
         }
     }
