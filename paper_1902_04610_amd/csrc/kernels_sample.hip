@@ -7,14 +7,14 @@
 // Every limit keeps a beginning of the order, so nothing is sorted: the place of a token in the order is a 52-bit number (the logit's bits, made
 // monotonous, in front of the index), and a limit is the number of the last token that is kept.
 //
-// Two kernels.  Reading the logits once would take 9 us for 256 rows of 128256 bf16; this takes 86 with rows of all kinds of limits (16 for one row of 32000 floats):
+// Two kernels.  Reading the logits once would take 9 us for 256 rows of 128256 bf16; this takes 84 with rows of all kinds of limits (16 for one row of 32000 floats):
 //   slice_rows    a workgroup takes 8192 logits of a row and leaves their first token, their sum of weights if the row wants it, and the places of
 //                 those that a limit may keep, in order of index: all down to a threshold that at least so many of its threads' largest logits reach as
 //                 the limit may want of one slice; for top_p also the weight in bins of 1 / 16 of a power of two.  Bound by its vector instructions: 18 us
 //                 for greedy rows, 27 with lists, 40 with 64-bit weights, 56 with bins.
 //   choose_rows   a workgroup per row puts that together.  Without limits it reads one slice again (10 us); where the kept tokens all lie above every
 //                 slice's threshold, which the lists tell, none (8 - 20).  Else it finds the bin in which top_p ends, reads the row once for that bin's tokens, and one
-//                 slice again for the token (45 for one such row: one compute unit's latencies and instructions, a chain of some ten barriers); with min_p too it
+//                 slice again for the token (43 for one such row: one compute unit's latencies and instructions, a chain of some ten barriers); with min_p too it
 //                 reads the row again for the kept weight of sixteen runs.
 // What even that does not hold (lists that run over: thousands of equal logits, top_k beyond them) is found by reading the row several times
 // (choose_anywhere), eleven bits of the last place at a time by histograms of how many tokens there are, or how much weight.
