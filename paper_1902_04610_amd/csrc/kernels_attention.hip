@@ -2,7 +2,7 @@
 //
 //   y = sum_t w_t v_t / sum_t w_t,  w_t = 2^(scale log2(e) q . k_t - m),  m the largest so far, sums scaled when it grows
 //
-// Few rows: bound by reading the cache once (1.9 GB of two jobs' four sequences of 115000 keys 300 us, 6.3 TB/s; 285 MB of 136 sequences of 1 .. 6000 keys 75 us).  A workgroup takes sixteen columns, a key head and a part of the keys, its four wavefronts tiles of 32 keys by turns
+// Few rows: bound by reading the cache once (1.9 GB of two jobs' four sequences of 115000 keys 300 us, 6.3 TB/s; 285 MB of 90 sequences of 1 .. 6000 keys 75 us).  A workgroup takes sixteen columns, a key head and a part of the keys, its four wavefronts tiles of 32 keys by turns
 // (v_mfma_f32_16x16x32_bf16); the parts of a long sequence are joined by a second kernel.
 #include <algorithm>
 #include <vector>
@@ -22,7 +22,7 @@ constexpr int32_t kStride = 4 * (int32_t)kKeys;      // keys between two tiles o
 
 // Few rows, one sequence of 8 key heads of 128, us for 500 / 1000 / 4000 / 16000 keys: parts of 256 10.6 11.1 11.4 19.9, of 512 8.4 12.3 12.6 18.9, of 1024 8.4
 // 10.8 16.5 19.5: up to kWhole keys a second launch costs more than it saves.  16 such sequences, 1000 / 2000 keys: 18.5 28.9, 20.7 28.5, 16.2 32.6; 16 jobs,
-// 136 sequences of 1 .. 6000 keys: 80, 67, 63.  The rule knows the job alone, not the call's others: what a job is answered does not depend on its neighbours.
+// 90 sequences of 1 .. 6000 keys: 80, 67, 63.  The rule knows the job alone, not the call's others: what a job is answered does not depend on its neighbours.
 // Prompts and chunks: a workgroup fills a compute unit, and what the rule cannot know (rows are a bound, jobs are several) makes more than one round of them likely.
 // us with 512 / 256 / 192 workgroups wanted: chunks of 512 behind 8000 .. 20000 keys, a window of 4096, 102 96 78; of 512 behind 8000 120 96 107; a prompt of 2048 92 64
 // 63; 256 behind 16000 58 75 81; 11 such shapes 0.91 and 0.88 of the time of 512.
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(kAttentionThreads, N <= 4 ? 2 : 1) void attend_few(
 // travel straight into LDS, as they lie in the cache, two stages ahead (v_mfma_f32_32x32x16_bf16; every read from LDS is 512 consecutive bytes for each half of
 // the lanes).  One barrier a stage: what it says is that all of the stage has landed and that the stage before it has been read.
 // The largest score is only followed when it grows by more than 2^8: sums stay far below the largest float, and are scaled hardly ever.
-// 12 prompts of 1000 - 5000 rows, 32 heads of 128: 465 us, 0.86 PFLOP/s; a tile of a wavefront takes some 950 cycles, 512 of them multiplies.
+// 12 prompts of 1000 - 2700 rows, 32 heads of 128: 465 us, 0.86 PFLOP/s; a tile of a wavefront takes some 950 cycles, 512 of them multiplies.
 constexpr float kGrowth = 8.0f;
 
 // Sixteen bytes a lane from base + from + off to LDS at `to` + 16 lane.  The scalars may come from lane reads: five wait states stand in front of their use.
