@@ -301,8 +301,9 @@ __device__ inline void slice_row(const SampleProblem &p, uint32_t r, uint32_t sl
                 if (reached <= want + want / 4) break;
             }
         }
-        // nothing that min_p keeps lies below this (the margin is for the roundings of this line)
-        if (q.min_p > 0.0f) {
+        // nothing that min_p keeps lies below this (the margin is for the roundings of this line; infinity has none: infinity less infinity is no number, whose place
+        // among the keys its sign would decide)
+        if (q.min_p > 0.0f && top != INFINITY) {
             const float below = q.temperature * logf(q.min_p);
             down_to = max(down_to, key_of(top + below - 1e-5f * (fabsf(top) + fabsf(below))));
         }
