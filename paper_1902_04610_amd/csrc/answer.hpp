@@ -38,7 +38,8 @@ struct AttentionProblem {
 };
 struct AttentionParts { uint32_t columns, part, parts; };
 AttentionParts attention_parts(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len, uint32_t window);
-uint64_t attention_work_floats(uint32_t M, uint32_t Hq, uint32_t D, const AttentionParts &);
+uint64_t attention_work_floats(uint32_t M, uint32_t Hq, uint32_t D, const AttentionParts &);      // that a call uses
+uint64_t attention_room_floats(uint32_t M, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len);      // at least that of calls of up to M rows and max_len tokens
 hipError_t launch_attention(const AttentionProblem *p, uint32_t n, hipStream_t stream, uint64_t *launches);
 
 struct SampleProblem {

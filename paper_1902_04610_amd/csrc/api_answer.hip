@@ -85,7 +85,9 @@ int32_t attention(salus_pool_t *pool, const salus_attention_desc *descs, uint32_
         if (const char *wrong = cache_wrong(d)) return wrong;
         if (d.max_len == 0 || d.max_len > (uint64_t)d.max_pages * d.page || d.max_len >= 1u << 30) return "max_len must be positive, below 2^30 and at most max_pages * page";
         if (!(d.scale > 0.0f) || !std::isfinite(d.scale)) return "scale must be positive and finite";
-        const uint64_t M = d.M, cache = salus_cache_bytes(d.n_pages, d.Hkv, d.page, d.D), work = salus_attention_work_bytes(d.M, d.n_seqs, d.Hq, d.Hkv, d.D, d.max_len);
+        const uint64_t M = d.M, cache = salus_cache_bytes(d.n_pages, d.Hkv, d.page, d.D),
+                       // what this call uses, which may be less than the room that the host function wants for it and all smaller ones
+                       work = up256(4 * attention_work_floats(d.M, d.Hq, d.D, attention_parts(d.M, d.n_seqs, d.Hq, d.Hkv, d.D, d.max_len, 0)));
         Ranges persist(at.P), lane(at.lane_size);
         persist.read(d.k_off, cache);
         persist.read(d.v_off, cache);
@@ -168,7 +170,7 @@ int32_t salus_grouped_append(salus_pool_t *pool, const salus_append_desc *descs,
 uint64_t salus_attention_work_bytes(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len)
 {
     if (!heads_ok(Hq, Hkv, D) || !seqs_ok(M, n_seqs, Hq, Hkv) || max_len == 0 || max_len >= 1u << 30) return 0;
-    return up256(4 * attention_work_floats(M, Hq, D, attention_parts(M, n_seqs, Hq, Hkv, D, max_len, 0)));
+    return up256(4 * attention_room_floats(M, Hq, Hkv, D, max_len));
 }
 
 int32_t salus_grouped_attention(salus_pool_t *pool, const salus_attention_desc *descs, uint32_t n, void *stream)

@@ -54,6 +54,19 @@ uint64_t attention_work_floats(uint32_t M, uint32_t Hq, uint32_t D, const Attent
     return parts.parts == 1 ? 0 : (uint64_t)M * Hq * parts.parts * (D + 2);
 }
 
+// What a call uses goes up and down with its rows, sequences and tokens: 64 rows of 32 heads of 128 behind 130000 tokens 14 MB, 63 of them 26, 4096 none.  A job's lane is
+// laid out once, so its room is a bound that never falls.  With t tiles of c columns, T wanted: there are several parts only for t < T, no more than max_len / 512 rounded up and
+// no more than (T / t) (513 / 512) + 1 (a part's keys are max_len t / T, rounded down where that is 512 or more); columns of all heads are fewer than c t.  So columns times
+// parts are fewer than c T (513 / 512) + c t, and t is below T.
+uint64_t attention_room_floats(uint32_t M, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len)
+{
+    if (max_len <= kWhole) return 0;
+    const auto most = [](uint64_t columns, uint64_t target) { return columns * target * 1025 / 512; };
+    uint64_t sums = most(kFewColumns, kFewTarget);
+    if ((uint64_t)M * (Hq / Hkv) >= kManyFrom) sums = std::max(sums, most(many_columns(D), kManyTarget));
+    return std::min(sums, (uint64_t)M * Hq * (((uint64_t)max_len + kLeastPart - 1) / kLeastPart)) * (D + 2);
+}
+
 // A tile of 32 keys, D = 32 N elements a head.  Lane 16 g + c: of row c of K's fragment t, k-step i, elements 32 i + 8 g .. + 8 of key 8 (c / 4) + 4 t + c % 4;
 // of V's fragment i element 16 i + c of tokens 8 g .. + 8.
 template <int N>

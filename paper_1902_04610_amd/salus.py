@@ -550,6 +550,7 @@ def cache_bytes(n_pages, Hkv, page, D):
 
 
 def attention_work_bytes(M, n_seqs, Hq, Hkv, D, max_len):
+    """Room for all rounds of up to M rows, n_seqs sequences and max_len tokens."""
     return lib().salus_attention_work_bytes(*_whole(M=M, n_seqs=n_seqs, Hq=Hq, Hkv=Hkv, D=D, max_len=max_len))
 
 
