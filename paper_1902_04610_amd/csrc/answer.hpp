@@ -73,7 +73,7 @@ inline hipError_t launch_answer_of(void (*kernel)(AnswerArgs<P, NP>), int thread
         AnswerArgs<P, NP> a{};
         const uint64_t total = fill_group(a, p + at, n - at < NP ? n - at : NP, tiles);
         if (total > 0x7fffffffull) return hipErrorInvalidValue;
-        const hipError_t e = launch_tiles(total, launches, [&](uint32_t blocks, uint32_t base) {
+        const hipError_t e = launch_tiles(total, threads, launches, [&](uint32_t blocks, uint32_t base) {
             a.base = base;
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, stream, a);
         });

@@ -33,14 +33,15 @@ struct BlockFewArgs {
     BlockProblem p[kBlockFew];
 };
 
-// A grid has fewer than 2^32 threads: kernels of one tile per workgroup, which have 256, take more tiles in several launches (of a multiple of 8, for the XCDs).
-// launch(workgroups, first tile).
-constexpr uint64_t kMostBlocks = 1u << 23;
+// A grid has fewer than 2^32 threads: kernels of one tile per workgroup, of `threads` threads (a power of two), take more tiles in several launches (of a multiple of 8, for
+// the XCDs).  launch(workgroups, first tile).
+constexpr uint64_t kMostThreads = 1u << 31;
 template <typename Launch>
-inline hipError_t launch_tiles(uint64_t tiles, uint64_t *launches, Launch launch)
+inline hipError_t launch_tiles(uint64_t tiles, int threads, uint64_t *launches, Launch launch)
 {
-    for (uint64_t base = 0; base < tiles; base += kMostBlocks) {
-        launch((uint32_t)(tiles - base < kMostBlocks ? tiles - base : kMostBlocks), (uint32_t)base);
+    const uint64_t most = kMostThreads / threads;
+    for (uint64_t base = 0; base < tiles; base += most) {
+        launch((uint32_t)(tiles - base < most ? tiles - base : most), (uint32_t)base);
         if (launches) *launches += 1;
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

@@ -45,7 +45,7 @@ inline hipError_t launch_block(void (*kernel)(Args), int threads, uint32_t bm, u
         const uint64_t tiles = fill_group(a, p + at, std::min(kMost, n - at),
                                           [&](const BlockProblem &q) { return (uint64_t)((q.M + bm - 1) / bm) * ((q.N + cols - 1) / cols); });
         if (tiles > 0x7fffffffull) return hipErrorInvalidValue;
-        const hipError_t e = launch_tiles(grid ? std::min<uint64_t>(tiles, grid) : tiles, launches, [&](uint32_t blocks, uint32_t base) {
+        const hipError_t e = launch_tiles(grid ? std::min<uint64_t>(tiles, grid) : tiles, threads, launches, [&](uint32_t blocks, uint32_t base) {
             a.base = base;
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, stream, a);
         });

@@ -297,7 +297,7 @@ hipError_t launch_block_slope(const SlopeProblem *p, uint32_t n, hipStream_t str
             return q.dZ || q.db ? (uint64_t)((q.M + kSlopeRows - 1) / kSlopeRows) * ((q.N + kSlopeCols - 1) / kSlopeCols) : 0;
         });
         if (tiles > 0x7fffffffull) return hipErrorInvalidValue;
-        const hipError_t e = launch_tiles(tiles, launches, [&](uint32_t blocks, uint32_t base) {
+        const hipError_t e = launch_tiles(tiles, 256, launches, [&](uint32_t blocks, uint32_t base) {
             a.base = base;
             hipLaunchKernelGGL(block_slope, dim3(blocks), dim3(256), 0, stream, a);
         });
