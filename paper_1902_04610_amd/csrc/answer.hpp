@@ -65,14 +65,19 @@ constexpr uint32_t kAnswerProblems = 24;
 static_assert(sizeof(AnswerArgs<AppendProblem, kAnswerProblems>) <= 4096 && sizeof(AnswerArgs<AttentionProblem, kAnswerProblems>) <= 4096,
               "kernel arguments are limited to 4 KB");
 
-// Runs n problems through launches of as many as fit: kernel(args) of `threads` threads a workgroup, one for each of tiles(problem).
+// Runs n problems through launches of as many as fit, by their arguments and by their tiles, which have 31-bit numbers: kernel(args) of `threads` threads a workgroup, one for
+// each of tiles(problem).
 template <typename P, uint32_t NP, typename Tiles>
 inline hipError_t launch_answer_of(void (*kernel)(AnswerArgs<P, NP>), int threads, const P *p, uint32_t n, hipStream_t stream, uint64_t *launches, Tiles tiles)
 {
-    for (uint32_t at = 0; at < n; at += NP) {
+    for (uint32_t at = 0, count = 0; at < n; at += count) {
         AnswerArgs<P, NP> a{};
-        const uint64_t total = fill_group(a, p + at, n - at < NP ? n - at : NP, tiles);
-        if (total > 0x7fffffffull) return hipErrorInvalidValue;
+        count = n - at < NP ? n - at : NP;
+        uint64_t total;
+        while ((total = fill_group(a, p + at, count, tiles)) > 0x7fffffffull) {
+            if (count == 1) return hipErrorInvalidValue;
+            count = (count + 1) / 2;
+        }
         const hipError_t e = launch_tiles(total, threads, launches, [&](uint32_t blocks, uint32_t base) {
             a.base = base;
             hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, stream, a);
@@ -81,7 +86,6 @@ inline hipError_t launch_answer_of(void (*kernel)(AnswerArgs<P, NP>), int thread
     }
     return hipSuccess;
 }
-
 
 // A tile of a sequence's rows.
 struct SequenceTile {

@@ -99,3 +99,9 @@ def test_few_columns_and_appends_of_millions_of_sequences(tmp_path):
     check(launches(tmp_path, "attention", 1, dict(CACHED, M=n, n_seqs=n, Hq=1, Hkv=1, D=32)), "attend_few", n // 16 + n)
     sizes = {k: v for k, v in CACHED.items() if k != "max_len"}
     check(launches(tmp_path, "append", 1, dict(sizes, M=n, n_seqs=n, Hq=1, Hkv=1, D=32)), "append_rows", n // 8 + 2 * n)
+
+
+def test_jobs_whose_workgroups_no_launch_numbers_together(tmp_path):
+    n, jobs = 60_000_000, 30
+    sizes = {k: v for k, v in CACHED.items() if k != "max_len"}
+    check(launches(tmp_path, "append", jobs, dict(sizes, M=1, n_seqs=n, Hq=1, Hkv=1, D=32)), "append_rows", jobs * 2 * n)
