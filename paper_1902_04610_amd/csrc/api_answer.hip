@@ -84,7 +84,8 @@ int32_t attention(salus_pool_t *pool, const salus_attention_desc *descs, uint32_
     const int32_t rc = for_jobs(pool, descs, n, [&](const salus_attention_desc &d, const Placed &at) -> const char * {
         if (const char *wrong = cache_wrong(d)) return wrong;
         if (d.max_len == 0 || d.max_len > (uint64_t)d.max_pages * d.page || d.max_len >= 1u << 30) return "max_len must be positive, below 2^30 and at most max_pages * page";
-        if (!(d.scale > 0.0f) || !std::isfinite(d.scale)) return "scale must be positive and finite";
+        const float scale = d.scale * 1.4426950408889634f;       // of powers of two
+        if (!(d.scale > 0.0f) || !std::isfinite(scale)) return "scale must be positive, and finite times log2(e)";
         const uint64_t M = d.M, cache = salus_cache_bytes(d.n_pages, d.Hkv, d.page, d.D),
                        // what this call uses, which may be less than the room that the host function wants for it and all smaller ones
                        work = up256(4 * attention_work_floats(d.M, d.Hq, d.D, attention_parts(d.M, d.n_seqs, d.Hq, d.Hkv, d.D, d.max_len, 0)));
@@ -100,7 +101,7 @@ int32_t attention(salus_pool_t *pool, const salus_attention_desc *descs, uint32_
         if (lane.overlap()) return kOverlap;
         const AttentionParts parts = attention_parts(d.M, d.n_seqs, d.Hq, d.Hkv, d.D, d.max_len, d.window);
         problems.push_back({seq, at.lane + d.q_off, at.persist + d.k_off, at.persist + d.v_off, at.lane + d.y_off,
-                            work ? (float *)(at.lane + d.work_off) : nullptr, d.max_len, d.window, d.scale * 1.4426950408889634f, parts.part, parts.parts, parts.columns});
+                            work ? (float *)(at.lane + d.work_off) : nullptr, d.max_len, d.window, scale, parts.part, parts.parts, parts.columns});
         return nullptr;
     });
     if (rc) return rc;

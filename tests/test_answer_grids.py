@@ -39,7 +39,7 @@ else:
     if kind == "append":
         sizes = dict(sizes, rotary=0, layout=0, magnitude=1.0, freq_off=s.ABSENT)
     else:
-        sizes = dict(sizes, window=0, scale=0.1, work_off=0)
+        sizes = dict(dict(window=0, scale=0.1, work_off=0), **sizes)
 pool = s.Pool(1 << 50, up(jobs * (P + E)), max_lanes=jobs, stream=0x50, policy=s.POLICY_PACK)
 ids = []
 for _ in range(jobs):
@@ -58,7 +58,8 @@ print(json.dumps([rc, pool.last_error(), take().decode().splitlines()]))
 """
 
 
-def launches(so_dir, kind, jobs, sizes):
+def call(so_dir, kind, jobs, sizes):
+    """Status, message, what was launched."""
     if not os.path.exists(build.LIB):
         build.build()
     so = str(so_dir / "librecorder.so")
@@ -66,7 +67,11 @@ def launches(so_dir, kind, jobs, sizes):
     env = dict(os.environ, LD_PRELOAD=":".join(filter(None, [so, os.environ.get("LD_PRELOAD")])), PYTHONPATH=build.ROOT)
     r = subprocess.run([sys.executable, "-c", CHILD, json.dumps([kind, jobs, sizes])], cwd=build.ROOT, env=env, stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
     assert r.returncode == 0, r.stderr[-3000:]
-    rc, error, lines = json.loads(r.stdout.splitlines()[-1])
+    return json.loads(r.stdout.splitlines()[-1])
+
+
+def launches(so_dir, kind, jobs, sizes):
+    rc, error, lines = call(so_dir, kind, jobs, sizes)
     assert rc == 0, (rc, error)
     return [(name, int(grid), int(block)) for name, grid, block in
             (re.match(r"launch \S*?(attend_few|attend_many|join_parts|append_rows|slice_rows|choose_rows)\S* (\d+) (\d+) \S+$", line).groups() for line in lines)]
