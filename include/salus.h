@@ -442,7 +442,7 @@ int32_t salus_grouped_clip_sgd(salus_pool_t *pool, const salus_clip_desc *descs,
  *
  * The new rows of a round and the sequences they belong to lie in the job's lane as int32 arrays, read on the device (a recorded call takes
  * what they hold when it is replayed): starts, n_seqs + 1 entries that do not fall, sequence s has rows starts[s] .. starts[s + 1] - 1 of M (none
- * is fine; M Hq + 32 n_seqs Hkv is below 2^31); lens, its tokens with the new ones, so that its n rows are its last n tokens; table, max_pages entries a sequence, the page
+ * is fine; M Hq + 32 n_seqs Hkv is below 2^31); lens, its tokens with the new ones (below 2^30), so that its n rows are its last n tokens; table, max_pages entries a sequence, the page
  * of token t is table[s][t / page].  Entries behind a sequence's last page are not used.  Rows in no sequence are neither read nor written.  What a device array
  * should not hold is harmless: rows outside 0 .. M are left out, tokens in pages outside 0 .. n_pages - 1 are neither stored nor seen,
  * rows in front of token 0 are not stored and see nothing. */
@@ -502,7 +502,7 @@ int32_t salus_grouped_attention(salus_pool_t *pool, const salus_attention_desc *
  * is its random number.  With w = exp((logit - largest) / temperature), kept are of that order
  *     the first top_k (0 and below: all),  of these the fewest from the front whose w reach top_p of their sum,  of these those with w >= min_p,
  * at least the first, and the token is the smallest index up to which the sum of the kept w, in order of index, exceeds u times the sum of all kept.  Temperature 0 and below (or NaN): the first
- * of the order.  top_p of 1 and above or NaN, min_p of 0 and below or NaN: no limit; u is cut to [0, 1).  A NaN counts as minus infinity; where nothing is larger, the token is -1.
+ * of the order; infinite: the largest float.  top_p of 1 and above or NaN, min_p of 0 and below or NaN: no limit; u is cut to [0, 1).  A NaN counts as minus infinity; where nothing is larger, the token is -1.
  * Weights are in 64 bits, to 1e-11 of themselves or 2^-44 of the largest, and summed in an order that does not change: the same call gives the same tokens.  tokens: M int32, written. work:
  * salus_sample_work_bytes().  V is at least 1 and at most 2^19. */
 typedef struct {

@@ -3,7 +3,8 @@
 // A column is one (row, query head) of a sequence and a key head; the columns of a key head follow each other row by row, its query heads fastest, so that heads
 // that share keys fill a tile.  S^T = K Q^T puts a column into one lane of each group of lanes, and with them its scores; these are, rounded to bf16, the second
 // operand of O^T = V^T P^T as they are: the contraction runs over keys in any order as long as V's is the same, and K's rows are taken in the
-// order that gives a lane the eight consecutive keys whose values lie together in the cache.  Nothing but the join of the wavefronts passes through LDS.
+// order that gives a lane the eight consecutive keys whose values lie together in the cache.  Scores and weights never pass through LDS: attend_few has the join of its wavefronts there,
+// attend_many the keys and values that its wavefronts share.
 #pragma once
 #include "answer.hpp"
 

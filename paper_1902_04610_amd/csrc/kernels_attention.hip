@@ -26,6 +26,7 @@ constexpr int32_t kStride = 4 * (int32_t)kKeys;      // keys between two tiles o
 // Prompts and chunks: a workgroup fills a compute unit, and what the rule cannot know (rows are a bound, jobs are several) makes more than one round of them likely.
 // us with 512 / 256 / 192 workgroups wanted: chunks of 512 behind 8000 .. 20000 keys, a window of 4096, 102 96 78; of 512 behind 8000 120 96 107; a prompt of 2048 92 64
 // 63; 256 behind 16000 58 75 81; 11 such shapes 0.91 and 0.88 of the time of 512.
+// (Parts are asked for with kLeastPart keys at least; that many are then evened out and rounded up to 128: 1025 keys are three of 384.)
 constexpr uint32_t kWhole = 1024, kLeastPart = 512, kFewTarget = 512, kManyTarget = 192;
 
 AttentionParts attention_parts(uint32_t M, uint32_t n_seqs, uint32_t Hq, uint32_t Hkv, uint32_t D, uint32_t max_len, uint32_t window)
@@ -82,7 +83,7 @@ struct FewLoads {
     const AttentionProblem &p;
     const Global<int32_t> *table;
     uint32_t head, k_at, v_at;
-    int32_t first, end;          // this wavefront's first key, the part's end
+    int32_t first;               // this wavefront's first key
     int32_t pages, pages_from;   // lane l: page of the tile that begins at pages_from + l kStride
 
     __device__ void load(int32_t key, FewTile<N> &t)
@@ -125,7 +126,7 @@ struct FewSums {
     }
 
     // all: every column sees every key of the tile.  end: the first key that none sees.
-    __device__ void add(FewTile<N> &t, const u32x4 (&q)[N], float scale, Sight sight, bool all, int32_t end, const AttentionProblem &p, const FewLoads<N> &loads)
+    __device__ void add(FewTile<N> &t, const u32x4 (&q)[N], float scale, Sight sight, bool all, int32_t end)
     {
         const uint32_t lane = threadIdx.x & 63, g = lane >> 4;
         f32x4 x[2] = {};
@@ -164,7 +165,7 @@ struct FewSums {
                 special |= any_special(t.v[i]);
             }
             if (__any(special)) {
-                add_seen(t, x, sight, p, loads);
+                add_seen(t, x, sight);
                 return;
             }
         }
@@ -175,7 +176,7 @@ struct FewSums {
 
     // O^T += V^T P^T key by key, leaving out what a column does not see.  The values come from the lanes that hold them: element 16 i + 4 g + e of a key in
     // tokens 8 k .. + 8 is with lane 16 k + 4 g + e.
-    __device__ void add_seen(const FewTile<N> &t, const f32x4 (&x)[2], Sight sight, const AttentionProblem &, const FewLoads<N> &)
+    __device__ void add_seen(const FewTile<N> &t, const f32x4 (&x)[2], Sight sight)
     {
         const uint32_t lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
 #pragma unroll 1
@@ -230,10 +231,10 @@ __global__ __launch_bounds__(kAttentionThreads, N <= 4 ? 2 : 1) void attend_few(
     for (int k = 0; k < 2 * N; ++k) s.o[k] = f32x4{};
     const int32_t from = tile.key + (int32_t)(tile.part * p.part), end = min(tile.key_end, from + (int32_t)p.part);
     FewLoads<N> loads{p, (const Global<int32_t> *)p.seq.table + (uint64_t)tile.s * p.seq.max_pages, tile.head,
-                      (g * 32 + (c / 4) * 8 + c % 4) * 16, (g * D + c) * 16, from + (int32_t)(kKeys * wave), end, 0, INT32_MIN};
+                      (g * 32 + (c / 4) * 8 + c % 4) * 16, (g * D + c) * 16, from + (int32_t)(kKeys * wave), 0, INT32_MIN};
     const auto add = [&](FewTile<N> &tile_of) {
         const bool all = tile_of.key > every.low && tile_of.key + 31 <= every.high;
-        s.add(tile_of, q, p.scale, sight, all, tile.key_end, p, loads);
+        s.add(tile_of, q, p.scale, sight, all, tile.key_end);
     };
     if constexpr (TWO) {
         FewTile<N> one, two;
@@ -310,7 +311,8 @@ __global__ __launch_bounds__(kAttentionThreads, N <= 4 ? 2 : 1) void attend_few(
 // Prompts and chunks of them: bound by the matrix pipes and by what the exponentials leave of them.  A workgroup's wavefronts have 32 columns each and share the tiles of keys and values, which
 // travel straight into LDS, as they lie in the cache, two stages ahead (v_mfma_f32_32x32x16_bf16; every read from LDS is 512 consecutive bytes for each half of
 // the lanes).  One barrier a stage: what it says is that all of the stage has landed and that the stage before it has been read.
-// The largest score is only followed when it grows by more than 2^8: sums stay far below the largest float, and are scaled hardly ever.
+// The largest score is only followed when it grows by more than 2^8 (lazy rescaling, a published method for running softmax sums): sums stay far below the largest float, and are
+// scaled hardly ever.  Up to D = 128 the next tile's scores are multiplied while the weights of this one are made; from 192 on the sums leave no registers for that, and the two follow each other.
 // 12 prompts of 1000 - 2700 rows, 32 heads of 128: 465 us, 0.86 PFLOP/s; a tile of a wavefront takes some 950 cycles, 512 of them multiplies.
 constexpr float kGrowth = 8.0f;
 

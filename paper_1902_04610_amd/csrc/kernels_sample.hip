@@ -114,26 +114,19 @@ struct LogitRow {
     }
 };
 
-// A token's place in the order, 52 bits: larger is earlier.
-constexpr uint32_t kPlaceBits = 52;
-__device__ inline uint64_t place_of(float x, uint32_t index)
-{
-    const uint32_t b = __builtin_bit_cast(uint32_t, x);
-    return (uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 20 | (0xfffffu - index);
-}
-__device__ inline uint32_t index_of(uint64_t place) { return 0xfffffu - ((uint32_t)place & 0xfffffu); }
-__device__ inline float logit_of(uint64_t place)
-{
-    const uint32_t b = (uint32_t)(place >> 20);
-    return __builtin_bit_cast(float, b & 0x80000000u ? b & 0x7fffffffu : ~b);
-}
-
+// A float's bits, made monotonous.
 __device__ inline uint32_t key_of(float x)
 {
     const uint32_t b = __builtin_bit_cast(uint32_t, x);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ inline float float_of(uint32_t key) { return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+
+// A token's place in the order, 52 bits: larger is earlier.
+constexpr uint32_t kPlaceBits = 52;
+__device__ inline uint64_t place_of(float x, uint32_t index) { return (uint64_t)key_of(x) << 20 | (0xfffffu - index); }
+__device__ inline uint32_t index_of(uint64_t place) { return 0xfffffu - ((uint32_t)place & 0xfffffu); }
+__device__ inline float logit_of(uint64_t place) { return float_of((uint32_t)(place >> 20)); }
 
 // 2^(d per), the product from -64 to 0, to 1e-11 of itself: the series of 2^f = e^(f ln 2) up to f^9 on [-1/2, 1/2], whose next term is below (ln 2 / 2)^10 / 10! = 7e-12;
 // 3 2^51 rounds to whole numbers, which then stand in the lowest bits.
@@ -170,12 +163,11 @@ struct RowLimits : Weights {
     uint64_t cut;                // place of the last token that is kept by top_k and top_p
     double min_p;
     __device__ RowLimits(uint64_t first_place, float temperature, float min) : Weights(logit_of(first_place), temperature), first(first_place), cut(0), min_p((double)min) {}
-    __device__ double weight(float x) const { return of(x); }
     __device__ uint64_t units(double w) const { return (uint64_t)(w * kWeightUnit + 0.5); }
     __device__ uint64_t kept(float x, uint32_t index) const
     {
         if (place_of(x, index) < cut || x == -INFINITY) return 0;
-        const double w = weight(x);
+        const double w = of(x);
         return w >= min_p ? units(w) : 0;
     }
 };
@@ -520,7 +512,7 @@ __device__ inline uint64_t reach(const Each &each, const RowLimits &l, bool by_w
             if (left < kPlaceBits && place >> left != prefix) return;
             const uint32_t bin = kBins - 1 - ((uint32_t)(place >> rest) & ((1u << bits) - 1));
             atomicAdd(&c.count[bin], 1u);
-            if (by_weight) atomicAdd(&c.mass[bin], (unsigned long long)l.units(l.weight(logit_of(place))));
+            if (by_weight) atomicAdd(&c.mass[bin], (unsigned long long)l.units(l.of(logit_of(place))));
         });
         __syncthreads();
         // two bins a thread, the earliest tokens in front
@@ -576,7 +568,7 @@ __device__ inline int32_t choose_anywhere(const LogitRow &row, const RowParams &
         uint64_t total = 0;
         for (uint32_t i = threadIdx.x; i < row.V; i += kSampleThreads) {
             const float x = row[i];
-            total += x != -INFINITY && place_of(x, i) >= l.cut ? l.units(l.weight(x)) : 0;
+            total += x != -INFINITY && place_of(x, i) >= l.cut ? l.units(l.of(x)) : 0;
         }
         total = block_total(total, c);
         l.cut = max(l.cut, reach_in_row(row, l, true, min(q.share((double)total), total), c));
@@ -636,7 +628,7 @@ __device__ inline int32_t choose_listed(uint32_t count, const RowParams &q, RowL
     l.min_p = 0;             // (for the sums)
     // everything there is is known, or everything that min_p keeps
     const bool everything = down_to <= key_of(-INFINITY) + 1;
-    bool known = everything || (min_p > 0.0 && l.weight(float_of(down_to)) < min_p);
+    bool known = everything || (min_p > 0.0 && l.of(float_of(down_to)) < min_p);
     uint64_t cut = (uint64_t)down_to << 20;
     const auto each = [&](const auto &f) {
 #pragma unroll 1
@@ -658,7 +650,7 @@ __device__ inline int32_t choose_listed(uint32_t count, const RowParams &q, RowL
     }
     if (q.top_p < 1.0f) {
         uint64_t weight = 0;
-        each([&](uint64_t place) { weight += l.units(l.weight(logit_of(place))); });
+        each([&](uint64_t place) { weight += l.units(l.of(logit_of(place))); });
         weight = block_total(weight, c);
         const bool all = everything || q.top_k;      // these are all that share the weight
         const uint64_t target = all ? min(q.share((double)weight), weight) : q.share(total);
@@ -704,7 +696,7 @@ __device__ inline bool find_bin(const RowWork &work, const RowLimits &l, const S
 {
     static_assert(kMassBins <= kSampleThreads && kMassBins % 64 == 0, "a bin a thread");
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const double factor = mine.first ? l.weight(logit_of(mine.first)) : 0.0;
+    const double factor = mine.first ? l.of(logit_of(mine.first)) : 0.0;
     if (__any(lane < work.slices && mine.first && !mine.binned)) return false;
     double sum = 0;
     if (threadIdx.x < kMassBins) {
@@ -819,7 +811,7 @@ __device__ inline bool cut_in_bin(const LogitRow &row, const RowParams &q, RowLi
     each([&](uint64_t place) {
         most = max(most, place);
         least = max(least, ~place);
-        weight += l.units(l.weight(logit_of(place)));
+        weight += l.units(l.of(logit_of(place)));
     });
     weight = block_total(weight, c);
     if (weight == 0) return false;
@@ -854,7 +846,7 @@ __device__ inline int32_t choose_row(const SampleProblem &p, uint32_t r, ChooseS
     if (first == 0) return -1;
     if (q.greedy()) return (int32_t)index_of(first);
     RowLimits l(first, q.temperature, q.min_p);
-    double mass = mine.first && q.wants_mass() ? mine.mass * l.weight(logit_of(mine.first)) : 0.0;
+    double mass = mine.first && q.wants_mass() ? mine.mass * l.of(logit_of(mine.first)) : 0.0;
     if (q.limited()) {
         const double total = wave_total(mass) * kWeightUnit;
         const uint32_t count = gather_lists(work, mine, c);

@@ -60,20 +60,32 @@ def rounds():
     return out
 
 
-@pytest.fixture(scope="module")
-def outcomes(tmp_path_factory):
+def record(folder, asked):
+    """[(heads, largest round, call), (status, room of the largest, room of its own, launches)] for each call."""
     if not os.path.exists(build.LIB):
         build.build()
-    so = str(tmp_path_factory.mktemp("recorder") / "librecorder.so")
+    so = str(folder / "librecorder.so")
     subprocess.check_call(["gcc", "-O1", "-fPIC", "-shared", "-Wall", "-o", so, os.path.join(HERE, "launch_recorder.c")])
     env = dict(os.environ, LD_PRELOAD=":".join(filter(None, [so, os.environ.get("LD_PRELOAD")])), PYTHONPATH=build.ROOT)
-    asked = rounds()
     r = subprocess.run([sys.executable, "-c", CHILD], cwd=build.ROOT, env=env, input=json.dumps(asked), stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True)
     assert r.returncode == 0, r.stderr[-3000:]
     each = [(heads, most, call) for heads, most, smaller in asked for call in smaller]
     got = json.loads(r.stdout.splitlines()[-1])
     assert len(got) == len(each)
     return list(zip(each, got))
+
+
+@pytest.fixture(scope="module")
+def outcomes(tmp_path_factory):
+    return record(tmp_path_factory.mktemp("recorder"), rounds())
+
+
+def parts_of(heads, call, line):
+    (Hq, Hkv, D), (M, S, L, window) = heads, call
+    kernel, grid = re.match(r"launch \S*?(attend_few|attend_many)\S* (\d+) ", line).groups()
+    tiles = (M * (Hq // Hkv) // (16 if kernel == "attend_few" else 256 if D <= 128 else 128) + S) * Hkv
+    assert int(grid) % tiles == 0
+    return int(grid) // tiles
 
 
 def test_every_smaller_round_has_room_where_the_largest_has(outcomes):
@@ -84,9 +96,7 @@ def test_every_smaller_round_has_room_where_the_largest_has(outcomes):
 def test_the_sums_of_the_parts_fit(outcomes):
     several = 0
     for ((Hq, Hkv, D), most, (M, S, L, window)), (rc, work, own, lines) in outcomes:
-        kernel, grid = re.match(r"launch \S*?(attend_few|attend_many)\S* (\d+) ", lines[0]).groups()
-        columns = 16 if kernel == "attend_few" else 256 if D <= 128 else 128
-        parts = int(grid) // ((M * (Hq // Hkv) // columns + S) * Hkv)
+        parts = parts_of((Hq, Hkv, D), (M, S, L, window), lines[0])
         several += parts > 1
         assert parts == 1 or 4 * M * Hq * parts * (D + 2) <= own, (Hq, Hkv, D, most, M, S, L, window, parts)
     assert several > 200
@@ -108,3 +118,17 @@ def test_room_never_falls_as_a_round_grows(heads):
                 more = [M, n, L]
                 more[axis] = steps[at + 1]
                 assert bytes_ <= room[tuple(more)], (M, n, L, more)
+
+
+# (t tiles; several parts are asked for with at least 512 keys, then evened out and rounded up to 128)
+EXACT = [((4, 2, 64), (1, 1, 1024, 0), 1), ((4, 2, 64), (1, 1, 1025, 0), 3),              # t = 2: 3 of 384, two whole and 257 keys
+         ((4, 2, 64), (1, 1, 40000, 0), 79),                                              # 79 of 512
+         ((2, 1, 64), (3, 1, 3000, 1000), 3), ((2, 1, 64), (3, 1, 3000, 980), 1),         # a span of 1000 + 8 + 32 keys: 3 of 384; of 1020
+         ((8, 8, 256), (500, 1, 20000, 4096), 7),                                         # t = 32: 4256 keys by 709 are 7, of 640
+         ((8, 8, 256), (500, 1, 20000, 0), 7),                                            # by 3333, of 2944
+         ((16, 16, 64), (3000, 1, 3000, 0), 1), ((16, 16, 64), (2800, 1, 3000, 0), 2)]    # t = 192, as many as are wanted; 176: by 2750, 2 of 1536
+
+
+def test_the_number_of_parts(tmp_path):
+    for ((heads, _, call), (rc, _, _, lines)), (_, _, parts) in zip(record(tmp_path, [(heads, call[:3], [call]) for heads, call, _ in EXACT]), EXACT):
+        assert rc == salus.OK and parts_of(heads, call, lines[0]) == parts, (heads, call, lines)
