@@ -483,7 +483,8 @@ int32_t salus_grouped_append(salus_pool_t *pool, const salus_append_desc *descs,
  *     y = sum_t w_t v_t / sum_t w_t,   w_t = exp(scale q . k_t),   over tokens t <= p, with a window only p - window < t,
  * zero if it sees none.  A token that a row does not see does not reach it, whatever its key and value hold.  q, y: M x Hq D bf16 in the lane; scale positive, and
  * finite times log2(e); window 0: none.  Weights are rounded to bf16 as factors of the second product; a score beyond the largest float is none.  max_len: no sequence of the round is longer (longer ones are taken as of that
- * length); it bounds the launch, so that one recorded with max_len = max_pages page serves all lengths.  work:
+ * length); it bounds the launch, so that one recorded with max_len = max_pages page serves all lengths (parts of keys follow
+ * it: a bound of 131072 over lengths of some thousands takes 2 - 4 times as long).  work:
  * salus_attention_work_bytes() (0: work_off is ignored), which never falls as M, n_seqs or max_len grow: what is laid out for the largest of each
  * serves all rounds of the job.  max_len is below 2^30. */
 typedef struct {
